@@ -343,6 +343,89 @@ int conf_kv_step_static(conf_kv_handle *h, const float *dev_logits, float *dev_c
  */
 int conf_kv_evict_compact(conf_kv_handle *h, conf_kv_stream stream);
 
+/* Type of the values a model hands over. */
+typedef enum conf_kv_type {
+  CONF_KV_TYPE_FP32 = 0,     /* IEEE binary32 */
+  CONF_KV_TYPE_FP16 = 1,     /* IEEE binary16 */
+  CONF_KV_TYPE_BF16 = 2      /* the upper half of a binary32 */
+} conf_kv_type;
+
+/* Arguments of conf_kv_prepare_qkv.  Strides count values, are not negative and may be anything the alignment allows (a
+ * projection's fused row [Hq + 2 Hkv][D] is read where it is); the heads of a token are dense. */
+typedef struct conf_kv_qkv {
+  int32_t tokens;            /* T >= 0 per sequence; 0: nothing is done                                     */
+  int32_t type;              /* conf_kv_type of dev_q, dev_k, dev_v                                         */
+  const void *dev_q;         /* [B][T][Hq][D]                                                               */
+  const void *dev_k;         /* [B][T][Hkv][D]                                                              */
+  const void *dev_v;         /* [B][T][Hkv][D]                                                              */
+  int64_t q_batch_stride, q_token_stride;
+  int64_t k_batch_stride, k_token_stride;
+  int64_t v_batch_stride, v_token_stride;
+  const float *dev_q_weight; /* fp32 [D], or NULL: queries are not normalised                               */
+  const float *dev_k_weight; /* fp32 [D], or NULL: keys are not normalised                                  */
+  const float *dev_freq;     /* fp32 [rotated / 2]: angle per position of each pair                         */
+  const int32_t *dev_pos;    /* int32 [B][T] positions, or NULL: token t has the position that the next
+                                token appended to the layer gets, plus t, for every sequence                */
+  int32_t first;             /* added to every position (a shared prefix's tokens, say)                     */
+  int32_t rotated;           /* leading channels that turn: 0 .. D, a multiple of 16                        */
+  int32_t interleaved;       /* 0: pair p is channels (p, p + rotated / 2); 1: channels (2 p, 2 p + 1)      */
+  int32_t prompt_layout;     /* 0: keys and values [B][T][Hkv][D]; 1: [B][Hkv][T][D] (conf_kv_load_prefill) */
+  float eps;                 /* of the norm; finite, >= 0                                                   */
+  void *dev_q16;             /* fp16 [B][T][Hq][D], written                                                 */
+  void *dev_k16;             /* fp16, written                                                               */
+  void *dev_v16;             /* fp16, written                                                               */
+} conf_kv_qkv;
+
+/*
+ * Queries, keys and values as a projection leaves them, made into what conf_kv_attend, conf_kv_attend_chunk,
+ * conf_kv_attend_shared, conf_kv_observe* (queries; keys and values in decode layout) and conf_kv_load_prefill (prompt
+ * layout) take, in one pass.  Each query and key head x of a token becomes
+ *     y = x / sqrt(mean(x^2) + eps) * weight           (where a weight is given, else y = x)
+ *     (a, b) <- (a cos t - b sin t, b cos t + a sin t) for the pairs of its first `rotated` channels, t = position * freq
+ * and is rounded to fp16 once; values are rounded to fp16.  Angles are formed in float64, norms and products in float32.  What
+ * is beyond fp16's range becomes infinite.  Each of q, k and v may be left out (source and destination NULL), not all.
+ * The handle gives B, Hq, Hkv, D and, with dev_pos NULL, the positions, which live on the device: a recorded call moves on
+ * with the cache.  Nothing of the cache changes.  Tensors are 16-byte aligned and so are the strides in bytes; destinations
+ * overlap no source.  B * T at most 2^30. */
+int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *args, conf_kv_stream stream);
+
+/* Arguments of conf_kv_constrain.  NULL leaves a part out. */
+typedef struct conf_kv_constraints {
+  int32_t type;                     /* conf_kv_type of dev_logits                                              */
+  int32_t max_tokens;               /* most tokens of a row of dev_tokens that are read                        */
+  const void *dev_logits;           /* [B][V], rows logits_stride values apart                                 */
+  int64_t logits_stride;            /* >= V                                                                    */
+  float *dev_out;                   /* fp32 [B][V], written; may be dev_logits itself (fp32, stride V)         */
+  const int32_t *dev_tokens;        /* int32 [B][..]: every row's history, prompt first, then what was
+                                       generated; ids outside [0, V) count for nothing                         */
+  int64_t tokens_stride;            /* >= max_tokens                                                           */
+  const int32_t *dev_lengths;       /* int32 [B]: tokens of the row's history (0 .. max_tokens; taken as such)  */
+  const int32_t *dev_prompt_lengths;/* int32 [B]: how many of them are the prompt; NULL: none                  */
+  const float *dev_repetition;      /* fp32 [B], r > 0: logits of tokens in the history: x > 0 ? x / r : x * r  */
+  const float *dev_presence;        /* fp32 [B]: subtracted where the token was generated                      */
+  const float *dev_frequency;       /* fp32 [B]: subtracted as often as the token was generated                */
+  const int32_t *dev_bias_offsets;  /* int32 [B + 1]: row b's biases are entries offsets[b] .. offsets[b + 1]-1 */
+  const int32_t *dev_bias_tokens;   /* int32 [n_bias]                                                          */
+  const float *dev_bias_values;     /* fp32 [n_bias]: added (-inf bans a token); of several entries of one row
+                                       for one token the last one counts                                       */
+  int32_t n_bias;                   /* entries there are; offsets are held within 0 .. n_bias                  */
+  int32_t n_masks;                  /* rows of dev_allowed                                                     */
+  const uint32_t *dev_allowed;      /* uint32 [n_masks][ceil(V / 32)]: bit v & 31 of word v / 32 set = allowed  */
+  const int32_t *dev_allowed_rows;  /* int32 [B]: the mask row of each sequence, one outside 0 .. n_masks - 1
+                                       (-1): no mask; NULL: row b, n_masks >= B                                */
+} conf_kv_constraints;
+
+/*
+ * Logits made into what conf_kv_step takes: penalties for repeated tokens, then biases, then a grammar's mask, which puts
+ * -inf wherever it forbids (whatever was there, NaN included).  Each row's steps in this order:
+ *     x <- x > 0 ? x / repetition : x * repetition       where the token is in the history
+ *     x <- x - frequency * count - presence               where it was generated, count times
+ *     x <- x + bias;   x <- -inf where it is forbidden
+ * in float32.  (Nothing happens to the history's tokens with max_tokens 0.)  A row that forbids everything is all -inf; conf_kv_step then gives a confidence that is NaN and the loose
+ * budget.  Penalties need dev_tokens and dev_lengths; lengths, offsets, ids and mask rows are held within
+ * the arrays' bounds on the device.  The result does not depend on the order in which workgroups run. */
+int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_kv_stream stream);
+
 /*
  * Launch shapes for replayed steps (for callers that record a decode step into a HIP graph).
  * on != 0: from now on the split counts and kernel variants of conf_kv_attend* and

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -35,6 +36,12 @@ class ConfKVConfig(C.Structure):
         ("evict_page", C.c_int32), ("layout", C.c_int32),
     ]
 
+
+# conf_kv_qkv and conf_kv_constraints field by field (native alignment): packed into bytes, which a call hands over
+# faster than a ctypes.Structure with as many fields.
+_QKV = struct.Struct("@2i3P6q4P4if3P")
+_CONSTRAINTS = struct.Struct("@2iPqPPq8P2i2P")
+TYPE_FP32, TYPE_FP16, TYPE_BF16 = 0, 1, 2
 
 RANKERS = {"composite": 0, "random": 1}
 RANK_SCOPES = {"kv_head": 0, "layer": 1}
@@ -68,6 +75,8 @@ SYMBOLS = {
     "conf_kv_step": (C.c_int, [_P, _P, _P, _P, _P]),
     "conf_kv_step_static": (C.c_int, [_P, _P, _P, _P, _P]),
     "conf_kv_evict_compact": (C.c_int, [_P, _P]),
+    "conf_kv_prepare_qkv": (C.c_int, [_P, C.c_int32, C.c_char_p, _P]),
+    "conf_kv_constrain": (C.c_int, [_P, C.c_char_p, _P]),
     "conf_kv_static_plan": (C.c_int, [_P, C.c_int32]),
     "conf_kv_tag_state": (C.c_int, [_P, _P, _P, _P]),
     "conf_kv_lengths": (C.c_int, [_P, _P, _P]),
@@ -187,6 +196,7 @@ class ConfKV:
         if not torch.cuda.is_available():
             raise RuntimeError("ConfKV needs a GPU: the decode path has no CPU implementation")
         self._torch = torch
+        self._type = {torch.float32: TYPE_FP32, torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}
         self._current_stream = _stream_getter(torch)
         self.lib = load_library()
         self.cfg, self._nt, self._nl = make_config(**kw)
@@ -268,6 +278,86 @@ class ConfKV:
 
     def evict_compact(self):
         return self._check(self.lib.conf_kv_evict_compact(self.h, self._stream()), "conf_kv_evict_compact")
+
+    def _want(self, name: str, t, dtype, shape=None):
+        """The device pointer of a dense tensor that has to be as the call takes it (None: 0)."""
+        if t is None:
+            return 0
+        if t.dtype != dtype or (shape is not None and t.shape != shape) or not t.is_contiguous() or t.device != self.state.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor{'' if shape is None else f' of shape {tuple(shape)}'} on "
+                             f"{self.state.device} is wanted, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+        return t.data_ptr()
+
+    def _rows(self, name: str, t, like, heads: int):
+        """Pointer and strides of q, k or v [B][T][heads][D] with dense heads, of the type and tokens of `like`."""
+        if t is None:
+            return 0, 0, 0
+        c = self.cfg
+        if t.dtype != like.dtype or t.shape != (c.batch, like.shape[1], heads, c.head_dim) or t.device != self.state.device:
+            raise ValueError(f"{name}: {like.dtype} [{c.batch}][{like.shape[1]}][{heads}][{c.head_dim}] on {self.state.device} is "
+                             f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        sb, st, sh, sd = t.stride()
+        if t.numel() and (sd != 1 or (sh != c.head_dim and heads > 1)):
+            raise ValueError(f"{name}: the heads of a token are dense, got strides {t.stride()}")
+        return t.data_ptr(), sb if c.batch > 1 else 0, st if t.shape[1] > 1 else 0
+
+    def prepare_qkv(self, layer: int, q, k, v, q16=None, k16=None, v16=None, freq=None, pos=None, first: int = 0, q_weight=None,
+                    k_weight=None, eps: float = 1e-6, interleaved: bool = False, prompt: bool = False):
+        """Projection rows q [B][T][Hq][D], k and v [B][T][Hkv][D] (float32, float16 or bfloat16; slices of a fused row are
+        read where they are) -> q16 [B][T][Hq][D], k16 / v16 [B][T][Hkv][D], or [B][Hkv][T][D] with `prompt` (float16): RMS norm of
+        query and key heads (where a float32 weight [D] is given), rotation of the first 2 * len(freq) channels by
+        pos * freq, one rounding.  pos int32 [B][T], or None: the positions the next appended tokens of the layer get; `first` is
+        added.  Each of q, k and v may be None together with its destination."""
+        like = q if q is not None else k if k is not None else v
+        c = self.cfg
+        if like is None or like.dim() != 4 or like.dtype not in self._type:
+            raise ValueError("prepare_qkv: q, k or v [B][T][heads][D] of float32, float16 or bfloat16 is wanted")
+        B, T, H, D = c.batch, like.shape[1], c.n_kv_heads, c.head_dim
+        half = self._torch.float16
+        f32 = self._torch.float32
+        qp, qb, qt = self._rows("q", q, like, c.n_q_heads)
+        kp, kb, kt = self._rows("k", k, like, H)
+        vp, vb, vt = self._rows("v", v, like, H)
+        rows = (B, H, T, D) if prompt else (B, T, H, D)
+        args = _QKV.pack(T, self._type[like.dtype], qp, kp, vp, qb, qt, kb, kt, vb, vt, self._want("q_weight", q_weight, f32, (D,)),
+                         self._want("k_weight", k_weight, f32, (D,)), self._want("freq", freq, f32),
+                         self._want("pos", pos, self._torch.int32, (B, T)), first, 0 if freq is None else 2 * freq.numel(),
+                         bool(interleaved), bool(prompt), eps, self._want("q16", q16, half, (B, T, c.n_q_heads, D)),
+                         self._want("k16", k16, half, rows), self._want("v16", v16, half, rows))
+        return self._check(self.lib.conf_kv_prepare_qkv(self.h, layer, args, self._stream()), "conf_kv_prepare_qkv")
+
+    def constrain(self, logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
+                  frequency=None, bias_offsets=None, bias_tokens=None, bias_values=None, allowed=None, allowed_rows=None):
+        """logits [B][V] (float32, float16 or bfloat16, dense rows) -> out float32 [B][V], which may be `logits` itself.
+        tokens int32 [B][n] with lengths and prompt_lengths int32 [B]; repetition, presence, frequency float32 [B]; biases as
+        bias_offsets int32 [B + 1] into bias_tokens int32 and bias_values float32; allowed int32 (or uint32) [masks][ceil(V / 32)]
+        with allowed_rows int32 [B] or one mask row per sequence."""
+        c, torch = self.cfg, self._torch
+        B, V, want, i32, f32 = c.batch, c.vocab, self._want, torch.int32, torch.float32
+        if logits.dtype not in self._type or logits.shape != (B, V) or logits.device != self.state.device or logits.stride(1) != 1:
+            raise ValueError(f"logits: [{B}][{V}] of float32, float16 or bfloat16 with dense rows is wanted, got {logits.dtype} "
+                             f"{tuple(logits.shape)} strides {logits.stride()} on {logits.device}")
+        n = 0
+        if tokens is not None:
+            n = tokens.shape[1] if tokens.dim() == 2 else -1
+            if tokens.dtype != i32 or tokens.shape != (B, n) or tokens.device != self.state.device or (n > 1 and tokens.stride(1) != 1):
+                raise ValueError(f"tokens: int32 [{B}][n] with dense rows is wanted, got {tokens.dtype} {tuple(tokens.shape)}")
+        elif repetition is not None or presence is not None or frequency is not None:
+            raise ValueError("tokens: penalties need the history")
+        m = 0 if bias_tokens is None else bias_tokens.numel()
+        masks = 0 if allowed is None else allowed.shape[0]
+        if allowed is not None and allowed.dtype != i32:
+            allowed = allowed.view(i32)
+        row = (B,)
+        args = _CONSTRAINTS.pack(
+            self._type[logits.dtype], n, logits.data_ptr(), logits.stride(0) if B > 1 else V, want("out", out, f32, (B, V)),
+            0 if tokens is None else tokens.data_ptr(), (tokens.stride(0) if B > 1 else n) if n else 0,
+            want("lengths", lengths, i32, row), want("prompt_lengths", prompt_lengths, i32, row),
+            want("repetition", repetition, f32, row), want("presence", presence, f32, row), want("frequency", frequency, f32, row),
+            want("bias_offsets", bias_offsets, i32, (B + 1,)), want("bias_tokens", bias_tokens, i32, (m,)),
+            want("bias_values", bias_values, f32, (m,)), m, masks, want("allowed", allowed, i32, (masks, (V + 31) // 32)),
+            want("allowed_rows", allowed_rows, i32, row))
+        return self._check(self.lib.conf_kv_constrain(self.h, args, self._stream()), "conf_kv_constrain")
 
     def lengths(self):
         c = self.cfg

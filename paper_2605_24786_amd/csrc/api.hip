@@ -182,6 +182,7 @@ struct conf_kv_handle {
   bool evict_separate = false;      // CONF_KV_EVICT_ONE=0 at create (tests)
   int spin_limit = kSpinLimitDefault;   // CONF_KV_SPIN_LIMIT at create (tests of the expiry path)
   int last_hip = 0;
+  int device = 0;                   // the device that was current at create
 };
 
 #define CK_HIP(h, expr)                         \
@@ -215,6 +216,7 @@ int conf_kv_create(conf_kv_handle **out, const conf_kv_config *cfg, void *dev_st
   conf_kv_handle *h = new (std::nothrow) conf_kv_handle();
   if (!h) return CONF_KV_ERR_INVALID_ARG;
   h->cfg = *cfg;
+  if (hipGetDevice(&h->device) != hipSuccess) h->device = 0;      // (the copies below then fail)
   h->n_tight.assign(cfg->n_tight, cfg->n_tight + cfg->n_layers);
   h->n_loose.assign(cfg->n_loose, cfg->n_loose + cfg->n_layers);
   h->cfg.n_tight = h->n_tight.data();
@@ -519,6 +521,129 @@ int conf_kv_step_static(conf_kv_handle *h, const float *dev_logits, float *dev_c
   CK_HIP(h, launch_conf_reduce_static(h->cv, dev_logits, h->cfg.vocab, h->spin_limit, h->withhold, dev_conf, dev_sel,
                                       (double)h->cfg.tau, (double)h->cfg.w_entropy, (double)h->cfg.w_margin,
                                       (double)h->cfg.w_top, (hipStream_t)stream));
+  return CONF_KV_OK;
+}
+
+// A call launches on the current device, a handle's memory is on the one it was created on.
+static bool on_its_device(const conf_kv_handle *h) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == h->device;
+}
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+static size_t value_bytes(int type) { return type == CONF_KV_TYPE_FP32 ? 4 : 2; }
+
+int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *args, conf_kv_stream stream) {
+  if (!h || !args) return CONF_KV_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= h->cfg.n_layers) return CONF_KV_ERR_BAD_LAYER;
+  const conf_kv_qkv &q = *args;
+  const int B = h->cfg.batch, D = h->cfg.head_dim, T = q.tokens;
+  if (T < 0 || (long long)B * T > (1ll << 30) || q.type < CONF_KV_TYPE_FP32 || q.type > CONF_KV_TYPE_BF16)
+    return CONF_KV_ERR_INVALID_ARG;
+  if (q.rotated < 0 || q.rotated > D || q.rotated % 16 || (q.rotated > 0 && !q.dev_freq)) return CONF_KV_ERR_INVALID_ARG;
+  if ((q.dev_q_weight || q.dev_k_weight) && !(q.eps >= 0.f && q.eps <= 3.0e38f)) return CONF_KV_ERR_INVALID_ARG;
+  if (T == 0) return CONF_KV_OK;
+  struct Part { const void *src; void *dst; int heads; int64_t batch, token; };
+  const Part parts[3] = {{q.dev_q, q.dev_q16, h->cfg.n_q_heads, q.q_batch_stride, q.q_token_stride},
+                         {q.dev_k, q.dev_k16, h->cfg.n_kv_heads, q.k_batch_stride, q.k_token_stride},
+                         {q.dev_v, q.dev_v16, h->cfg.n_kv_heads, q.v_batch_stride, q.v_token_stride}};
+  const size_t vb = value_bytes(q.type);
+  int given = 0;
+  constexpr int64_t kMostStride = (int64_t)1 << 40;
+  for (const Part &p : parts) {
+    if (!p.src != !p.dst) return CONF_KV_ERR_INVALID_ARG;
+    if (!p.src) continue;
+    ++given;
+    if (p.batch < 0 || p.token < 0 || p.batch > kMostStride || p.token > kMostStride) return CONF_KV_ERR_INVALID_ARG;
+    if (((uintptr_t)p.src | (uintptr_t)p.dst | (uintptr_t)(p.batch * vb) | (uintptr_t)(p.token * vb)) & 15)
+      return CONF_KV_ERR_INVALID_ARG;
+  }
+  if (!given) return CONF_KV_ERR_INVALID_ARG;
+  for (const Part &d : parts) {
+    if (!d.dst) continue;
+    const size_t written = (size_t)B * T * d.heads * D * 2;
+    for (const Part &p : parts)
+      if (p.src && overlap(p.src, ((B - 1) * (size_t)p.batch + (T - 1) * (size_t)p.token + (size_t)p.heads * D) * vb, d.dst, written))
+        return CONF_KV_ERR_INVALID_ARG;
+  }
+  if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
+  PrepareLaunch a{};
+  a.q = q.dev_q;
+  a.k = q.dev_k;
+  a.v = q.dev_v;
+  a.q_batch = q.q_batch_stride;
+  a.q_token = q.q_token_stride;
+  a.k_batch = q.k_batch_stride;
+  a.k_token = q.k_token_stride;
+  a.v_batch = q.v_batch_stride;
+  a.v_token = q.v_token_stride;
+  a.wq = q.dev_q_weight;
+  a.wk = q.dev_k_weight;
+  a.freq = q.dev_freq;
+  a.pos = q.dev_pos;
+  a.next = h->cv.ctl + kCtlPos + layer;
+  a.first = q.first;
+  a.q16 = (__half *)q.dev_q16;
+  a.k16 = (__half *)q.dev_k16;
+  a.v16 = (__half *)q.dev_v16;
+  a.B = B;
+  a.tokens = T;
+  a.Hq = h->cfg.n_q_heads;
+  a.Hkv = h->cfg.n_kv_heads;
+  a.rotated = q.rotated;
+  a.interleaved = q.interleaved != 0;
+  a.prompt = q.prompt_layout != 0;
+  a.eps = q.eps;
+  CK_HIP(h, launch_prepare(a, D, q.type, (hipStream_t)stream));
+  return CONF_KV_OK;
+}
+
+int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_kv_stream stream) {
+  if (!h || !args) return CONF_KV_ERR_INVALID_ARG;
+  const conf_kv_constraints &c = *args;
+  const int B = h->cfg.batch, V = h->cfg.vocab;
+  if (!c.dev_logits || !c.dev_out || c.type < CONF_KV_TYPE_FP32 || c.type > CONF_KV_TYPE_BF16 || c.logits_stride < V)
+    return CONF_KV_ERR_INVALID_ARG;
+  const size_t vb = value_bytes(c.type);
+  if ((uintptr_t)c.dev_logits % vb || (uintptr_t)c.dev_out % 4) return CONF_KV_ERR_INVALID_ARG;
+  const bool in_place = c.dev_logits == c.dev_out && c.type == CONF_KV_TYPE_FP32 && c.logits_stride == V;
+  if (!in_place && overlap(c.dev_logits, ((B - 1) * (size_t)c.logits_stride + V) * vb, c.dev_out, (size_t)B * V * 4))
+    return CONF_KV_ERR_INVALID_ARG;
+  const bool penalties = c.dev_repetition || c.dev_presence || c.dev_frequency;
+  if (penalties && (c.max_tokens < 0 || (c.max_tokens > 0 && (!c.dev_tokens || !c.dev_lengths || c.tokens_stride < c.max_tokens))))
+    return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_bias_offsets && (c.n_bias < 0 || (c.n_bias > 0 && (!c.dev_bias_tokens || !c.dev_bias_values)))) return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_allowed && (c.n_masks < 0 || (!c.dev_allowed_rows && c.n_masks < B))) return CONF_KV_ERR_INVALID_ARG;
+  if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
+  ConstrainLaunch a{};
+  a.logits = c.dev_logits;
+  a.row_stride = c.logits_stride;
+  a.out = c.dev_out;
+  if (penalties && c.max_tokens > 0) {
+    a.tokens = c.dev_tokens;
+    a.lengths = c.dev_lengths;
+    a.prompt_lengths = c.dev_prompt_lengths;
+    a.token_stride = c.tokens_stride;
+    a.max_tokens = c.max_tokens;
+    a.repetition = c.dev_repetition;
+    a.presence = c.dev_presence;
+    a.frequency = c.dev_frequency;
+  }
+  if (c.dev_bias_offsets && c.n_bias > 0) {
+    a.bias_offsets = c.dev_bias_offsets;
+    a.bias_tokens = c.dev_bias_tokens;
+    a.bias_values = c.dev_bias_values;
+    a.n_bias = c.n_bias;
+  }
+  a.allowed = c.dev_allowed;
+  a.allowed_rows = c.dev_allowed_rows;
+  a.n_masks = c.n_masks;
+  a.B = B;
+  a.V = V;
+  CK_HIP(h, launch_constrain(a, c.type, (hipStream_t)stream));
   return CONF_KV_OK;
 }
 

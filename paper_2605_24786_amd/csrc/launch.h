@@ -32,6 +32,40 @@ constexpr int kSpinLimitDefault = 400000;   // polls (about a microsecond each) 
 // ---- probe.hip ----
 hipError_t launch_probe_read(const void *src, size_t bytes, unsigned *out, int workgroups, hipStream_t stream);
 
+// types of the rows a model hands over (conf_kv_type)
+constexpr int kTypeFp32 = 0, kTypeFp16 = 1, kTypeBf16 = 2;
+
+// ---- prepare.hip ----
+struct PrepareLaunch {
+  const void *q, *k, *v;                 // [B][tokens][heads][D], each may be null
+  long long q_batch, q_token, k_batch, k_token, v_batch, v_token;   // strides in values
+  const float *wq, *wk, *freq;           // norm weights (null: no norm), angles per position
+  const int32_t *pos;                    // [B][tokens], or null: *next + token
+  const unsigned *next;
+  long long first;                       // added to every position
+  __half *q16, *k16, *v16;
+  int B, tokens, Hq, Hkv;
+  int rotated, interleaved, prompt;
+  float eps;
+};
+hipError_t launch_prepare(const PrepareLaunch &a, int D, int type, hipStream_t stream);
+
+// ---- constrain.hip ----
+struct ConstrainLaunch {
+  const void *logits;
+  long long row_stride;
+  float *out;                            // [B][V]
+  const int32_t *tokens, *lengths, *prompt_lengths;
+  long long token_stride;
+  const float *repetition, *presence, *frequency;
+  const int32_t *bias_offsets, *bias_tokens;
+  const float *bias_values;
+  const uint32_t *allowed;
+  const int32_t *allowed_rows;
+  int B, V, max_tokens, n_bias, n_masks;
+};
+hipError_t launch_constrain(const ConstrainLaunch &a, int type, hipStream_t stream);
+
 // ---- attend.hip ----
 struct AttendPlan {
   int splits;        // workgroups per unit
