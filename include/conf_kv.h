@@ -110,6 +110,8 @@ typedef struct conf_kv_config {
                                 capacity must hold max(n_loose, protected_window + g - 1) plus
                                 the appended tokens                                            */
   int32_t layout;            /* conf_kv_layout: where the INT8 slots of a unit live              */
+  int32_t max_shared;        /* most tokens of a shared prefix that conf_kv_attend_shared may be given (sizes the scratch
+                                buffer: up to 64 partial results per query row); 0: no such calls */
 } conf_kv_config;
 
 typedef enum conf_kv_layout {
@@ -271,6 +273,29 @@ int conf_kv_attend(conf_kv_handle *h, int32_t layer, const void *dev_q16, const 
 int conf_kv_attend_chunk(conf_kv_handle *h, int32_t layer, int32_t tq, const void *dev_q16,
                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16,
                          conf_kv_stream stream);
+
+/* A prefix that sequences share (a system prompt, a document that many questions are asked about): its keys, rotated, and
+ * values, stored once for the whole batch, in no cache and in no budget. */
+typedef struct conf_kv_prefix {
+  const void *dev_k16;       /* fp16 [Hkv][tokens][D], kv-heads head_stride values apart                        */
+  const void *dev_v16;       /* the same                                                                       */
+  int64_t head_stride;       /* >= tokens * D, a multiple of 8                                                 */
+  int32_t tokens;            /* 0 .. max_shared; 0: the call is conf_kv_attend_chunk's                         */
+  const int32_t *dev_seen;   /* int32 [B]: sequence b sees the first dev_seen[b] of them (held within 0 .. tokens;
+                                0: none); NULL: all see all                                                    */
+} conf_kv_prefix;
+
+/* conf_kv_attend_chunk for sequences behind a shared prefix: tokens of the call attend what they see of the prefix, the
+ * cache and the call's own tokens up to themselves, in one softmax,
+ *     out[b][t][h] = sum_i p_i V_i,   p = softmax over prefix and cache of sm_scale * q . K_i,
+ * and the importance of the cached slots follows the probabilities of that softmax (what goes to the prefix goes to no slot:
+ * sum_i A_i = G minus the prefix's share).  The prefix's keys and values are read once for the whole batch.  Tensors, errors
+ * and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend); tq * n_q_heads / n_kv_heads at most 16, and more than
+ * max_shared tokens, a null or misaligned prefix are CONF_KV_ERR_INVALID_ARG.  Prefix tensors are 16-byte aligned.
+ * Positions are the caller's affair: the handle's count the cache only (conf_kv_prepare_qkv's `first` adds the prefix).
+ * conf_kv_observe* see the cache alone.  A recorded call keeps the prefix's place and length and reads dev_seen anew. */
+int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const conf_kv_prefix *prefix, const void *dev_q16,
+                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream);
 
 /* Importance from the prompt's own attention (the step before the decode loop: the cache's
  * initial importance comes from an observation window of queries at the end of the prompt

@@ -33,12 +33,13 @@ class ConfKVConfig(C.Structure):
         ("n_tight", C.POINTER(C.c_int32)), ("n_loose", C.POINTER(C.c_int32)),
         ("mass_gain", C.c_float), ("ranker", C.c_int32), ("rank_scope", C.c_int32),
         ("ranker_seed", C.c_uint64), ("scale_mode", C.c_int32), ("max_chunk", C.c_int32),
-        ("evict_page", C.c_int32), ("layout", C.c_int32),
+        ("evict_page", C.c_int32), ("layout", C.c_int32), ("max_shared", C.c_int32),
     ]
 
 
-# conf_kv_qkv and conf_kv_constraints field by field (native alignment): packed into bytes, which a call hands over
+# conf_kv_prefix, conf_kv_qkv and conf_kv_constraints field by field (native alignment): packed into bytes, which a call hands over
 # faster than a ctypes.Structure with as many fields.
+_PREFIX = struct.Struct("@2PqiP")
 _QKV = struct.Struct("@2i3P6q4P4if3P")
 _CONSTRAINTS = struct.Struct("@2iPqPPq8P2i2P")
 TYPE_FP32, TYPE_FP16, TYPE_BF16 = 0, 1, 2
@@ -70,6 +71,7 @@ SYMBOLS = {
     "conf_kv_load_prefill": (C.c_int, [_P, C.c_int32, _P, _P, C.c_int32, _P, _P]),
     "conf_kv_attend": (C.c_int, [_P, C.c_int32, _P, _P, _P, _P, _P]),
     "conf_kv_attend_chunk": (C.c_int, [_P, C.c_int32, C.c_int32, _P, _P, _P, _P, _P]),
+    "conf_kv_attend_shared": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_char_p, _P, _P, _P, _P, _P]),
     "conf_kv_observe": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
     "conf_kv_observe_prompt": (C.c_int, [_P, C.c_int32, _P, _P]),
     "conf_kv_step": (C.c_int, [_P, _P, _P, _P, _P]),
@@ -139,7 +141,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, vocab, capacit
                 protected_window, n_tight: Sequence[int], n_loose: Sequence[int], tau=0.7, alpha=0.65,
                 ema_decay=0.9, sm_scale=None, w_entropy=0.4, w_margin=0.3, w_top=0.3, mass_gain=None,
                 ranker="composite", rank_scope="kv_head", ranker_seed=0, scale_mode="token", max_chunk=0,
-                evict_page=0, layout="contiguous"):
+                evict_page=0, layout="contiguous", max_shared=0):
     """A ConfKVConfig plus the two int32 arrays it points to (keep the tuple alive)."""
     nt = (C.c_int32 * len(n_tight))(*[int(x) for x in n_tight])
     nl = (C.c_int32 * len(n_loose))(*[int(x) for x in n_loose])
@@ -150,7 +152,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, vocab, capacit
                        w_entropy, w_margin, w_top, nt, nl,
                        -1.0 if mass_gain is None else float(mass_gain), RANKERS[ranker],
                        RANK_SCOPES[rank_scope], int(ranker_seed), SCALE_MODES[scale_mode], int(max_chunk),
-                       int(evict_page), LAYOUTS[layout])
+                       int(evict_page), LAYOUTS[layout], int(max_shared))
     return cfg, nt, nl
 
 
@@ -246,6 +248,29 @@ class ConfKV:
         tq = int(q16.shape[1])
         return self._check(self.lib.conf_kv_attend_chunk(self.h, layer, tq, _ptr(q16), _ptr(knew16), _ptr(vnew16),
                                                          _ptr(out16), self._stream()), "conf_kv_attend_chunk")
+
+    def attend_shared(self, layer: int, q16, knew16, vnew16, out16, shared_k, shared_v, seen=None):
+        """q16 / out16 [B][tq][Hq][D], knew16 / vnew16 [B][tq][Hkv][D] as attend_chunk takes them, behind a prefix that the
+        sequences share: shared_k / shared_v float16 [Hkv][T][D] (a view of a longer buffer will do), of which sequence b sees
+        the first seen[b] tokens (int32 [B]; None: all)."""
+        c, half = self.cfg, self._torch.float16
+        H, D, tq = c.n_kv_heads, c.head_dim, int(q16.shape[1])
+        T = int(shared_k.shape[1])
+        for name, t in (("shared_k", shared_k), ("shared_v", shared_v)):
+            sh, st, sd = t.stride()
+            if t.dtype != half or t.shape != (H, T, D) or t.device != self.state.device or (t.numel() and (sd != 1 or (T > 1 and st != D))):
+                raise ValueError(f"{name}: float16 [{H}][{T}][{D}] with dense rows on {self.state.device} is wanted, got {t.dtype} "
+                                 f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+        stride = shared_k.stride(0) if H > 1 else T * D
+        if H > 1 and shared_v.stride(0) != stride:
+            raise ValueError("shared_k and shared_v: kv-heads equally far apart are wanted")
+        rows, new = (c.batch, tq, c.n_q_heads, D), (c.batch, tq, H, D)
+        want = self._want
+        prefix = _PREFIX.pack(shared_k.data_ptr(), shared_v.data_ptr(), stride, T,
+                              want("seen", seen, self._torch.int32, (c.batch,)))
+        return self._check(self.lib.conf_kv_attend_shared(self.h, layer, tq, prefix, want("q16", q16, half, rows),
+                                                          want("knew16", knew16, half, new), want("vnew16", vnew16, half, new),
+                                                          want("out16", out16, half, rows), self._stream()), "conf_kv_attend_shared")
 
     def observe(self, layer: int, first: int, q16, out16=None):
         """q16 / out16 [B][tq][Hq][D]: queries of the cached slots first .. first + tq - 1; out16 optional."""
@@ -433,6 +458,6 @@ def from_workload(wl, **override) -> ConfKV:
               ranker=getattr(wl, "ranker", "composite"), rank_scope=getattr(wl, "rank_scope", "kv_head"),
               ranker_seed=getattr(wl, "ranker_seed", 0), scale_mode=getattr(wl, "scale_mode", "token"),
               max_chunk=getattr(wl, "max_chunk", 0), evict_page=getattr(wl, "evict_page", 0),
-              layout=getattr(wl, "layout", "contiguous"))
+              layout=getattr(wl, "layout", "contiguous"), max_shared=getattr(wl, "max_shared", 0))
     kw.update(override)
     return ConfKV(**kw)

@@ -28,7 +28,7 @@ struct StateLayout {
 };
 
 struct ScratchLayout {
-  size_t conf_partial, part_ml, part_o, spill, score, src, sel, shared, total;
+  size_t conf_partial, part_ml, part_o, shared_ml, shared_o, spill, score, src, sel, shared, total;
   size_t zero_bytes;     // [0, zero_bytes) holds the counters and is zeroed at create
 };
 
@@ -58,7 +58,7 @@ bool config_ok(const conf_kv_config *c) {
   if (c->rank_scope != CONF_KV_SCOPE_KV_HEAD && c->rank_scope != CONF_KV_SCOPE_LAYER) return false;
   if (c->scale_mode != CONF_KV_SCALES_TOKEN && c->scale_mode != CONF_KV_SCALES_CHANNEL) return false;
   if (c->scale_mode == CONF_KV_SCALES_CHANNEL && (c->head_dim != 128 || c->fp16_window < 0)) return false;
-  if (c->max_chunk < 0) return false;
+  if (c->max_chunk < 0 || c->max_shared < 0) return false;
   // multi-token calls: one tile of 16 query rows per unit, or up to kWideRowsMax rows on the
   // many-rows kernel (per-token scales only)
   if (c->max_chunk > 1) {
@@ -140,6 +140,10 @@ ScratchLayout scratch_layout(const conf_kv_config *c) {
   // (the matrix-core body exchanges 128-channel partials whatever the head dimension)
   s.part_o = take(UPL * kAttendMaxSplits * R * std::max<size_t>(D, 128) * 8);
   s.zero_bytes = off;
+  // partial results of a shared prefix (rows of a call: at most 16 per unit)
+  const size_t parts = shared_parts_most(c->max_shared);
+  s.shared_ml = take(UPL * parts * R * sizeof(float2));
+  s.shared_o = take(UPL * parts * R * D * sizeof(float));
   // the two-launch form's scores, or the prompt-phase kernels' statistics; their parts also take the two arrays behind
   // this one, which only conf_kv_evict_compact uses
   s.spill = take(std::max(attend_spill_floats((int)UPL, (int)R, c->capacity),
@@ -363,7 +367,7 @@ static size_t table_lds(const conf_kv_handle *h) {
   return h->cv.page_lg ? ((size_t)h->cv.npages * 4 + 15) / 16 * 16 : 0;
 }
 
-static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan, int observe_first = -1) {
+static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan, int observe_first = -1, bool shared = false) {
   const bool observe = observe_first >= 0;
   const int n_ub = observe ? observe_first + tq : length_bound(h, layer) + tq;     // slots the call sees
   const int W = h->cfg.fp16_window;
@@ -378,17 +382,31 @@ static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan
   const bool rows16 = tq > 1 || observe || h->cv.G > 8;
   const int rows = rows16 ? kChunkRows : h->cv.G;
   if (!attend_plan(h->cfg.head_dim, rows, h->cv.chan != 0, h->cv.page_lg != 0, rows16, h->cfg.batch * h->cfg.n_kv_heads, n_ub, n16_ub,
-                   h->forced_splits, h->force_two_launch, table_lds(h), plan))
+                   h->forced_splits, h->force_two_launch, table_lds(h), shared, plan))
     return CONF_KV_ERR_BAD_SHAPE;
   // the paged layout is read by the single-launch matrix-core kernel only
   if (h->cv.page_lg && (plan->two_launch || !plan->mfma)) return CONF_KV_ERR_BAD_SHAPE;
   return CONF_KV_OK;
 }
 
-// observe_first < 0: append tq tokens and attend; >= 0: conf_kv_observe
+// A call launches on the current device, a handle's memory is on the one it was created on.
+static bool on_its_device(const conf_kv_handle *h) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == h->device;
+}
+
+static bool prefix_ok(const conf_kv_handle *h, int tq, const conf_kv_prefix *p) {
+  if (p->tokens < 0 || p->tokens > h->cfg.max_shared || tq * h->cv.G > kChunkRows) return false;
+  if (p->tokens == 0) return true;
+  if (!p->dev_k16 || !p->dev_v16 || (((uintptr_t)p->dev_k16 | (uintptr_t)p->dev_v16) & 15) || ((uintptr_t)p->dev_seen & 3)) return false;
+  return p->head_stride >= (int64_t)p->tokens * h->cfg.head_dim && p->head_stride % 8 == 0 && p->head_stride <= (int64_t)1 << 40 &&
+         on_its_device(h);
+}
+
+// observe_first < 0: append tq tokens and attend, prefix: with a shared prefix in front; >= 0: conf_kv_observe
 static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const void *dev_q16,
                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16,
-                         conf_kv_stream stream, int32_t observe_first = -1) {
+                         conf_kv_stream stream, int32_t observe_first = -1, const conf_kv_prefix *prefix = nullptr) {
   const bool observe = observe_first >= 0;
   if (!h || !dev_q16) return CONF_KV_ERR_INVALID_ARG;
   if (!observe && (!dev_knew16 || !dev_vnew16 || !dev_out16)) return CONF_KV_ERR_INVALID_ARG;
@@ -404,8 +422,10 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
     return CONF_KV_ERR_INVALID_ARG;
   if (h->appended[layer]) return CONF_KV_ERR_BAD_STATE;
   if (!observe && h->len_ub[layer] + tq > h->cfg.capacity) return CONF_KV_ERR_CAPACITY;
+  if (prefix && !prefix_ok(h, tq, prefix)) return CONF_KV_ERR_INVALID_ARG;
+  const bool shared = prefix && prefix->tokens > 0;
   AttendPlan plan;
-  int rc = plan_for_layer(h, layer, tq, &plan, observe_first);
+  int rc = plan_for_layer(h, layer, tq, &plan, observe_first, shared);
   if (rc != CONF_KV_OK) return rc;
   [[maybe_unused]] const size_t UPL = (size_t)h->cfg.batch * h->cfg.n_kv_heads;   // phase-trace builds
   AttendLaunch a{};
@@ -448,6 +468,32 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
     if (have >= region && need <= region) a.dbg = (unsigned long long *)(h->scratch + h->kl.total - region);
   }
 #endif
+  if (shared) {
+    SharedLaunch p{};
+    SharedPlan sp;
+    shared_plan(h->cfg.batch * tq * h->cv.G, h->cfg.n_kv_heads, prefix->tokens, device_cu_count(), &sp);
+    p.k = (const __half *)prefix->dev_k16;
+    p.v = (const __half *)prefix->dev_v16;
+    p.head_stride = prefix->head_stride;
+    p.seen = prefix->dev_seen;
+    p.q = a.q;
+    p.T = prefix->tokens;
+    p.B = h->cfg.batch;
+    p.Hkv = h->cfg.n_kv_heads;
+    p.G = h->cv.G;
+    p.tq = tq;
+    p.unit_rows = tq * h->cv.G;
+    p.parts = sp.parts;
+    p.part_keys = sp.part_keys;
+    p.sm_scale = h->cfg.sm_scale;
+    p.ml = (float2 *)(h->scratch + h->kl.shared_ml);
+    p.o = (float *)(h->scratch + h->kl.shared_o);
+    CK_HIP(h, launch_shared_prefix(p, sp, h->cfg.head_dim, (hipStream_t)stream));
+    a.shared_ml = p.ml;
+    a.shared_o = p.o;
+    a.shared_parts = p.parts;
+    a.shared_rows = p.unit_rows;
+  }
   CK_HIP(h, launch_attend(h->cv, a, plan, (hipStream_t)stream));
   if (!observe) {
     h->appended[layer] = (uint8_t)tq;
@@ -465,6 +511,12 @@ int conf_kv_attend_chunk(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16,
                          conf_kv_stream stream) {
   return attend_tokens(h, layer, tq, dev_q16, dev_knew16, dev_vnew16, dev_out16, stream);
+}
+
+int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const conf_kv_prefix *prefix, const void *dev_q16,
+                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream) {
+  if (!prefix) return CONF_KV_ERR_INVALID_ARG;
+  return attend_tokens(h, layer, tq, dev_q16, dev_knew16, dev_vnew16, dev_out16, stream, -1, prefix);
 }
 
 int conf_kv_observe(conf_kv_handle *h, int32_t layer, int32_t first, int32_t tq, const void *dev_q16,
@@ -522,12 +574,6 @@ int conf_kv_step_static(conf_kv_handle *h, const float *dev_logits, float *dev_c
                                       (double)h->cfg.tau, (double)h->cfg.w_entropy, (double)h->cfg.w_margin,
                                       (double)h->cfg.w_top, (hipStream_t)stream));
   return CONF_KV_OK;
-}
-
-// A call launches on the current device, a handle's memory is on the one it was created on.
-static bool on_its_device(const conf_kv_handle *h) {
-  int dev = -1;
-  return hipGetDevice(&dev) == hipSuccess && dev == h->device;
 }
 
 static bool overlap(const void *a, size_t na, const void *b, size_t nb) {

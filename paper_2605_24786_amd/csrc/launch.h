@@ -104,6 +104,10 @@ struct AttendLaunch {
   unsigned long long *dbg; // phase-trace buffer (CONFKV_TRACE builds), else null
   int tab_off;             // paged layout: byte offset of the unit's block table in dynamic LDS
   int trace_off;           // byte offset of the time stamps in dynamic LDS (CONFKV_TRACE builds)
+  // partial results of a shared prefix, which the wavefronts of a unit take in with their own (none: shared_parts = 0)
+  const float2 *shared_ml; // [units per layer][parts][rows] maximum and normaliser
+  const float *shared_o;   // [units per layer][parts][rows][D]
+  int shared_parts, shared_rows;
 };
 constexpr int kAttendMaxSplits = 64;
 constexpr int kChunkRows = 16;     // query rows per unit of a multi-token call (one matrix-core tile)
@@ -116,7 +120,7 @@ size_t attend_spill_floats(int units_per_layer, int G, int cap);   // scratch th
 // a multi-token call, which only has the single-launch matrix-core form).  Returns false when no plan fits the device.
 // extra_lds: bytes the launch needs behind the kernel's own dynamic LDS (the block table of the paged layout).
 bool attend_plan(int D, int G, bool chan, bool paged, bool chunk, int units_per_layer, int n_ub, int n16_ub, int forced_splits,
-                 bool force_two_launch, size_t extra_lds, AttendPlan *plan);
+                 bool force_two_launch, size_t extra_lds, bool shared /* a shared prefix is taken in */, AttendPlan *plan);
 // Plan of a call with more than kChunkRows query rows per unit (at most kWideRowsMax); false when
 // the shape cannot be served.  major_kv: kv-heads of the kv-head-first grid, 0 for the other.
 // n_ub: the most slots of a unit; n16_least, n16_ub: the fewest and the most FP16 ones.
@@ -125,6 +129,27 @@ int attend_wide_splits(int units_per_layer, int major_kv, int n_ub, int most, in
 bool attend_wide_plan(int rows, int units_per_layer, int major_kv, int n_ub, int n16_least, int n16_ub, int forced_splits, AttendPlan *plan);
 hipError_t launch_attend(const CacheView &cv, const AttendLaunch &a, const AttendPlan &plan,
                          hipStream_t stream);
+// ---- attend_shared.hip ----
+constexpr int kSharedMaxParts = 64;
+struct SharedPlan {
+  int row_waves;           // wavefronts of a workgroup side by side along the rows
+  int blocks;              // workgroups along the rows of a kv-head
+  int parts, part_keys;    // parts of the prefix and the keys of one
+};
+struct SharedLaunch {
+  const __half *k, *v;     // [Hkv][T][D], heads head_stride values apart
+  const __half *q;         // [B][tq][Hkv * G][D]
+  const int32_t *seen;     // [B] keys each sequence sees, or null: all
+  float2 *ml;              // [B * Hkv][parts][unit_rows]
+  float *o;                // [B * Hkv][parts][unit_rows][D]
+  long long head_stride;
+  int T, B, Hkv, G, tq, unit_rows /* tq * G */, parts, part_keys;
+  float sm_scale;
+};
+size_t shared_parts_most(int tokens);      // parts a prefix of up to that many tokens can be cut into
+void shared_plan(int rows, int Hkv, int T, int cus, SharedPlan *plan);
+int device_cu_count();
+hipError_t launch_shared_prefix(const SharedLaunch &a, const SharedPlan &p, int D, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,
 // contiguous layout).  scratch: scratch_floats floats, at least observe_scratch_floats(B * Hkv, G, T); with more the
 // work is cut into parts, observe_plan_floats(B * Hkv, G, T, first block of rows, INT8 slots, chan, scratch_floats, CUs) of them are used.
