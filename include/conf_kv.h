@@ -417,7 +417,7 @@ int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *arg
 /* Arguments of conf_kv_constrain.  NULL leaves a part out. */
 typedef struct conf_kv_constraints {
   int32_t type;                     /* conf_kv_type of dev_logits                                              */
-  int32_t max_tokens;               /* most tokens of a row of dev_tokens that are read                        */
+  int32_t max_tokens;               /* most tokens of a row of dev_tokens that are read, up to 2^30             */
   const void *dev_logits;           /* [B][V], rows logits_stride values apart                                 */
   int64_t logits_stride;            /* >= V                                                                    */
   float *dev_out;                   /* fp32 [B][V], written; may be dev_logits itself (fp32, stride V)         */
@@ -448,7 +448,7 @@ typedef struct conf_kv_constraints {
  *     x <- x + bias;   x <- -inf where it is forbidden
  * in float32.  (Nothing happens to the history's tokens with max_tokens 0.)  A row that forbids everything is all -inf; conf_kv_step then gives a confidence that is NaN and the loose
  * budget.  Penalties need dev_tokens and dev_lengths; lengths, offsets, ids and mask rows are held within
- * the arrays' bounds on the device.  The result does not depend on the order in which workgroups run. */
+ * the arrays' bounds on the device.  At most 2^27 logits a row (CONF_KV_ERR_BAD_SHAPE).  The result does not depend on the order in which workgroups run. */
 int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_kv_stream stream);
 
 /*

@@ -5,95 +5,240 @@
 //   x <- x - f_b n(v) - [n(v) > 0] p_b
 //   x <- x + bias_b(v)           (of several entries for one token the last one in the row's list counts)
 //   x <- allowed_b(v) ? x : -inf
-// A workgroup owns a range of the vocabulary of one row: it counts the row's history into LDS, keeping the tokens of its own
-// range (integer atomics, so that the order of arrival changes nothing), and then passes over its logits once.
+// A workgroup owns a range of the vocabulary of one row: it requests its logits and mask words, reads the row's whole history
+// meanwhile and counts the tokens of its own range in LDS (integer atomics, so that the order of arrival changes nothing),
+// applies the counts, reuses the LDS for the places of the biases, and writes its range once.
+#include <type_traits>
+
 #include "confkv_dev.h"
 #include "launch.h"
 
 namespace confkv {
 
-constexpr int kConThreads = 256;
-constexpr int kConPer = 16;
-constexpr int kConRange = kConThreads * kConPer;     // logits per workgroup
-constexpr unsigned kConSeen = 0x80000000u;           // the token occurs in the history; the other bits count its generated part
+constexpr int kConQuads = 4;                          // groups of four logits per thread
+constexpr unsigned kConSeen = 0x80000000u;            // the token occurs in the history; the other bits count its generated part
+
+typedef unsigned con_u4 __attribute__((ext_vector_type(4)));
 
 template <int kType>
-__device__ __forceinline__ float logit_at(const void *row, long long i) {
+__device__ __forceinline__ float logit_at(const void *row, int i) {
   if constexpr (kType == kTypeFp32) return ((const float *)row)[i];
   if constexpr (kType == kTypeFp16) return __half2float(((const __half *)row)[i]);
   return __uint_as_float((unsigned)((const unsigned short *)row)[i] << 16);
 }
-
+// four logits from a place aligned to them
 template <int kType>
-__global__ __launch_bounds__(kConThreads) void constrain_kernel(ConstrainLaunch a) {
-  __shared__ unsigned s_count[kConRange];
-  __shared__ int s_bias[kConRange];
-  const int b = blockIdx.y, tid = threadIdx.x;
-  const int lo = blockIdx.x * kConRange, size = min(kConRange, a.V - lo);
-  const char *row = (const char *)a.logits + (long long)b * a.row_stride * (kType == kTypeFp32 ? 4 : 2);
-  float x[kConPer];
+__device__ __forceinline__ void load_quad(const void *row, int i, float (&x)[4]) {
+  if constexpr (kType == kTypeFp32) {
+    const int4 v = ld_stream16((const float *)row + i);
+    x[0] = __int_as_float(v.x); x[1] = __int_as_float(v.y); x[2] = __int_as_float(v.z); x[3] = __int_as_float(v.w);
+  } else {
+    const confkv_v2u v = __builtin_nontemporal_load((const confkv_v2u *)((const unsigned short *)row + i));
 #pragma unroll
-  for (int k = 0; k < kConPer; ++k) x[k] = logit_at<kType>(row, min(lo + tid + k * kConThreads, a.V - 1));
-  const bool counts = a.tokens != nullptr, biases = a.bias_offsets != nullptr;
-  int b0 = 0, b1 = 0;
-  if (counts || biases) {
-    for (int i = tid; i < kConRange; i += kConThreads) {
-      s_count[i] = 0u;
-      s_bias[i] = 0;
+    for (int k = 0; k < 2; ++k) {
+      const unsigned w = k ? v.y : v.x;
+      if constexpr (kType == kTypeFp16) {
+        x[2 * k] = __half2float(__ushort_as_half((unsigned short)w));
+        x[2 * k + 1] = __half2float(__ushort_as_half((unsigned short)(w >> 16)));
+      } else {
+        x[2 * k] = __uint_as_float(w << 16);
+        x[2 * k + 1] = __uint_as_float(w & 0xffff0000u);
+      }
     }
-    __syncthreads();
-    if (counts) {
-      const int32_t *ids = a.tokens + (long long)b * a.token_stride;
-      const int n = min(max(a.lengths[b], 0), a.max_tokens), first = a.prompt_lengths ? a.prompt_lengths[b] : 0;
-      for (int i = tid; i < n; i += kConThreads) {
-        const unsigned at = (unsigned)(ids[i] - lo);
-        if (at < (unsigned)size) {
-          if (i < first) atomicOr(&s_count[at], kConSeen);
-          else atomicAdd(&s_count[at], 1u);
+  }
+}
+
+// A row's quads lie on 16-byte boundaries of the result: thread t's quad k is logits i .. i + 3 with i = lo + 4 (t + k kThreads),
+// lo = the range's start minus what the row is off such a boundary (so i may be -3 .. V - 1).  Where the logits of those
+// quads lie on boundaries too (same stride, or a fitting one) a quad is one load, else four.
+//
+// What bounds it: a call on a few rows is a chain -- arguments, lengths, the history, two barriers, the result -- so whatever can
+// be requested ahead of what it waits for is (first tokens of the history ahead of its length, biases ahead of the counts).  On
+// many rows it is the bytes of the logits and, with long histories, their re-reading by every range: ranges of 4096 logits for
+// short histories, of 8192 (half the re-reading, half the workgroups) from 8192 tokens on.  us with 4096 and 8192, BF16 logits,
+// biases and mask: 1 row of 128256 and 300 tokens 5.0, 5.2, 4096 tokens 6.5, 6.1, 32768 11.5, 9.0; 8 rows and 4096 tokens 6.6, 6.6; 32
+// rows and 4096 9.6, 9.8, 32768 16.6, 13.8 (16384 logits: 10.1, 13.3).  Rows are the grid's fast axis: with a multiple of eight
+// of them all ranges of a row run on one XCD, whose L2 then serves the history.
+// kWhole: every row consists of whole quads that lie on boundaries on both sides.
+template <int kType, int kThreads, bool kWhole>
+__global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) {
+  constexpr int kRange = kThreads * 4 * kConQuads;
+  constexpr int kValue = kType == kTypeFp32 ? 4 : 2;
+  __shared__ con_u4 s_slot[kRange / 4];
+  unsigned *slot = (unsigned *)s_slot;
+  const int b = blockIdx.x, tid = threadIdx.x, V = a.V;
+  float *out = a.out + (long long)b * V;
+  const int off = kWhole ? 0 : (int)(((uintptr_t)out >> 2) & 3);
+  const int lo = blockIdx.y * kRange - off;
+  const char *row = (const char *)a.logits + (long long)b * a.row_stride * kValue;
+  const bool quads = kWhole || (((uintptr_t)(row - off * kValue) & (4 * kValue - 1)) == 0 && V >= 8);
+  const int first_quad = (4 - off) & 3, last_quad = ((V - 4 + off) & ~3) - off;   // whole quads of the row: the first and the last
+  // ---- requests ----
+  float x[kConQuads][4];
+  if (quads) {
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k) load_quad<kType>(row, min(max(lo + 4 * (tid + k * kThreads), first_quad), last_quad), x[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(lo + 4 * (tid + k * kThreads) + e, 0), V - 1));
+  }
+  typename std::conditional<kWhole, unsigned, unsigned long long>::type bits[kConQuads];   // the quad's mask bits, and what lies behind them
+#pragma unroll
+  for (int k = 0; k < kConQuads; ++k) bits[k] = 15u;
+  if (a.allowed) {
+    const int m = a.allowed_rows ? a.allowed_rows[b] : b;
+    if (m >= 0 && m < a.n_masks) {
+      const int words = (V + 31) / 32;
+      const uint32_t *mask = a.allowed + (long long)m * words;
+#pragma unroll
+      for (int k = 0; k < kConQuads; ++k) {
+        // (a quad that starts ahead of the row takes its bits from the row's first word, moved up)
+        const int i = lo + 4 * (tid + k * kThreads), w = min(max(i, 0) >> 5, words - 1);
+        if constexpr (kWhole) {
+          bits[k] = mask[w] >> (i & 31);
+        } else {
+          const unsigned long long two = mask[w] | (unsigned long long)mask[min(w + 1, words - 1)] << 32;
+          bits[k] = i < 0 ? two << -i : two >> (i & 31);
         }
       }
     }
-    if (biases) {
-      b0 = min(max(a.bias_offsets[b], 0), a.n_bias);
-      b1 = min(a.bias_offsets[b + 1], a.n_bias);
-      for (int i = b0 + tid; i < b1; i += kConThreads) {
-        const unsigned at = (unsigned)(a.bias_tokens[i] - lo);
-        if (at < (unsigned)size) atomicMax(&s_bias[at], i - b0 + 1);
+  }
+  const int32_t *ids = a.tokens + (long long)b * a.token_stride;
+  const bool by_four = a.tokens && ((uintptr_t)ids & 15) == 0 && a.max_tokens >= 4;
+  int4 ahead = make_int4(0, 0, 0, 0);
+  if (by_four) ahead = ((const int4 *)ids)[min(tid, (a.max_tokens >> 2) - 1)];
+  int b0 = 0, b1 = 0, bias_ahead = -1;
+  if (a.bias_offsets) {
+    b0 = min(max(a.bias_offsets[b], 0), a.n_bias);
+    b1 = min(a.bias_offsets[b + 1], a.n_bias);
+    if (b0 + tid < b1) bias_ahead = a.bias_tokens[b0 + tid];
+  }
+  // the row's first and last quad where they are no whole ones (behind the requests: what is loaded twice is waited for)
+  if (!kWhole && quads) {
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k) {
+      const int i = lo + 4 * (tid + k * kThreads);
+      if (i < 0 || (i + 4 > V && i < V)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(i + e, 0), V - 1));
       }
+    }
+  }
+  const int n = a.tokens ? min(max(a.lengths[b], 0), a.max_tokens) : 0;
+  // slot s of the LDS is token lo + s
+  auto in_range = [&](int id, unsigned &at) {
+    at = (unsigned)id - (unsigned)lo;
+    return (unsigned)id < (unsigned)V && at < (unsigned)kRange;
+  };
+  // ---- the history's counts ----
+  if (n > 0) {
+    const int first = a.prompt_lengths ? a.prompt_lengths[b] : 0;
+    const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f;
+    const float freq = a.frequency ? a.frequency[b] : 0.f;
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    auto count = [&](int id, int i) {
+      unsigned at;
+      if (in_range(id, at)) {
+        if (i < first) atomicOr(&slot[at], kConSeen);
+        else atomicAdd(&slot[at], 1u);
+      }
+    };
+    auto count4 = [&](const int4 &v, int i) {
+      count(v.x, i);
+      count(v.y, i + 1);
+      count(v.z, i + 2);
+      count(v.w, i + 3);
+    };
+    int done = 0;
+    if (by_four) {
+      const int groups = n >> 2;
+      if (tid < groups) count4(ahead, 4 * tid);
+      for (int g0 = tid + kThreads; g0 < groups; g0 += 4 * kThreads) {
+        int4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = ((const int4 *)ids)[min(g0 + u * kThreads, groups - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int g = g0 + u * kThreads;
+          if (g >= groups) break;
+          count4(v[u], 4 * g);
+        }
+      }
+      done = groups << 2;
+    }
+    for (int i0 = done + tid; i0 < n; i0 += 8 * kThreads) {
+      int v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = ids[min(i0 + u * kThreads, n - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * kThreads < n) count(v[u], i0 + u * kThreads);
     }
     __syncthreads();
-  }
-  const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f;
-  const float freq = a.frequency ? a.frequency[b] : 0.f;
-  const uint32_t *mask = nullptr;
-  if (a.allowed) {
-    const int m = a.allowed_rows ? a.allowed_rows[b] : b;
-    if (m >= 0 && m < a.n_masks) mask = a.allowed + (long long)m * ((a.V + 31) / 32);
-  }
-  float *out = a.out + (long long)b * a.V;
 #pragma unroll
-  for (int k = 0; k < kConPer; ++k) {
-    const int i = tid + k * kConThreads;
-    if (i >= size) break;
-    float v = x[k];
-    if (counts) {
-      const unsigned s = s_count[i];
-      if (s != 0u) {
-        v = v > 0.f ? v / rep : v * rep;
-        const unsigned n = s & ~kConSeen;
-        if (n != 0u) v = v - freq * (float)n - pres;
+    for (int k = 0; k < kConQuads; ++k) {
+      const con_u4 s = s_slot[tid + k * kThreads];
+      if ((s.x | s.y | s.z | s.w) == 0u) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (s[e] == 0u) continue;
+        const float v = x[k][e] > 0.f ? x[k][e] / rep : x[k][e] * rep;
+        const unsigned c = s[e] & ~kConSeen;
+        x[k][e] = c != 0u ? v - freq * (float)c - pres : v;
       }
     }
-    if (biases && s_bias[i] != 0) v += a.bias_values[b0 + s_bias[i] - 1];
-    if (mask && !((mask[(lo + i) >> 5] >> ((lo + i) & 31)) & 1u)) v = -INFINITY;
-    out[lo + i] = v;
+  }
+  // ---- the row's biases ----
+  if (b0 < b1) {
+    // (a thread clears the slots that only it has read since the last barrier)
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    for (int i = b0 + tid; i < b1; i += kThreads) {
+      unsigned at;
+      if (in_range(i == b0 + tid ? bias_ahead : a.bias_tokens[i], at)) atomicMax(&slot[at], (unsigned)(i - b0 + 1));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kConQuads; ++k) {
+      const con_u4 s = s_slot[tid + k * kThreads];
+      if ((s.x | s.y | s.z | s.w) == 0u) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (s[e] != 0u) x[k][e] += a.bias_values[b0 + (int)s[e] - 1];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kConQuads; ++k) {
+    const int i = lo + 4 * (tid + k * kThreads);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[k][e] = (bits[k] >> e) & 1u ? x[k][e] : -INFINITY;
+    if (kWhole ? i < V : i >= 0 && i + 4 <= V) {
+      *(float4 *)(out + i) = make_float4(x[k][0], x[k][1], x[k][2], x[k][3]);
+    } else if (!kWhole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i + e >= 0 && i + e < V) out[i + e] = x[k][e];
+    }
   }
 }
 
 hipError_t launch_constrain(const ConstrainLaunch &a, int type, hipStream_t stream) {
-  const dim3 grid((a.V + kConRange - 1) / kConRange, a.B);
-  auto fn = type == kTypeFp32 ? constrain_kernel<kTypeFp32> : type == kTypeFp16 ? constrain_kernel<kTypeFp16> : constrain_kernel<kTypeBf16>;
-  hipLaunchKernelGGL(fn, grid, dim3(kConThreads), 0, stream, a);
+  const size_t value = type == kTypeFp32 ? 4 : 2;
+  const bool whole = a.V % 4 == 0 && a.row_stride % 4 == 0 && (uintptr_t)a.logits % (4 * value) == 0 && (uintptr_t)a.out % 16 == 0;
+  const int threads = a.tokens && a.max_tokens >= 8192 ? 512 : 256;
+  const int range = threads * 4 * kConQuads;
+  const dim3 grid(a.B, (a.V + 3 + range - 1) / range);     // (a row may start three places into its first quad)
+#define CONFKV_CASE(t, n) \
+  if (type == t && threads == n && whole) hipLaunchKernelGGL((constrain_kernel<t, n, true>), grid, dim3(n), 0, stream, a); \
+  if (type == t && threads == n && !whole) hipLaunchKernelGGL((constrain_kernel<t, n, false>), grid, dim3(n), 0, stream, a);
+  CONFKV_CASE(kTypeFp32, 256) CONFKV_CASE(kTypeFp16, 256) CONFKV_CASE(kTypeBf16, 256)
+  CONFKV_CASE(kTypeFp32, 512) CONFKV_CASE(kTypeFp16, 512) CONFKV_CASE(kTypeBf16, 512)
+#undef CONFKV_CASE
   return hipGetLastError();
 }
 
