@@ -16,6 +16,7 @@
 namespace confkv {
 
 constexpr int kConQuads = 4;                          // groups of four logits per thread
+constexpr int kConAhead = 4;                          // groups of four tokens per thread in flight
 constexpr unsigned kConSeen = 0x80000000u;            // the token occurs in the history; the other bits count its generated part
 
 typedef unsigned con_u4 __attribute__((ext_vector_type(4)));
@@ -48,18 +49,22 @@ __device__ __forceinline__ void load_quad(const void *row, int i, float (&x)[4])
   }
 }
 
-// A row's quads lie on 16-byte boundaries of the result: thread t's quad k is logits i .. i + 3 with i = lo + 4 (t + k kThreads),
-// lo = the range's start minus what the row is off such a boundary (so i may be -3 .. V - 1).  Where the logits of those
-// quads lie on boundaries too (same stride, or a fitting one) a quad is one load, else four.
+// A row's logits are counted from the 16-byte boundary of the result at or ahead of its first one (`off` places), so that quads
+// of them are one store each, and one load where the logits lie on boundaries likewise: thread t's quad k is logits i .. i + 3
+// with i = lo + 4 (t + k kThreads), lo = the range's start minus `off`.
+// kWhole: every row consists of whole quads that lie on boundaries on both sides.
 //
 // What bounds it: a call on a few rows is a chain -- arguments, lengths, the history, two barriers, the result -- so whatever can
 // be requested ahead of what it waits for is (first tokens of the history ahead of its length, biases ahead of the counts).  On
-// many rows it is the bytes of the logits and, with long histories, their re-reading by every range: ranges of 4096 logits for
-// short histories, of 8192 (half the re-reading, half the workgroups) from 8192 tokens on.  us with 4096 and 8192, BF16 logits,
-// biases and mask: 1 row of 128256 and 300 tokens 5.0, 5.2, 4096 tokens 6.5, 6.1, 32768 11.5, 9.0; 8 rows and 4096 tokens 6.6, 6.6; 32
-// rows and 4096 9.6, 9.8, 32768 16.6, 13.8 (16384 logits: 10.1, 13.3).  Rows are the grid's fast axis: with a multiple of eight
-// of them all ranges of a row run on one XCD, whose L2 then serves the history.
-// kWhole: every row consists of whole quads that lie on boundaries on both sides.
+// many rows it is the bytes of the logits and, with long histories, the vector ALU: every range passes over the row's whole
+// history, some seven instructions per token and wavefront.  So ranges of 4096 logits for short histories and of 8192 (half the
+// passes, half the workgroups) from 2048 tokens on.
+// us with 4096 and 8192 (BF16 logits, 64 biases, a mask): 1 row of 128256 and 300 tokens 4.9, 5.0, 4096 tokens 6.2, 5.9, 32768
+// 10.8, 8.1; 8 rows and 4096 tokens 6.4, 6.4; 32 rows and 300 tokens 8.4, 8.9, 32768 16.8, 13.7, no history 7.1, 7.4 (25 MB: 3.5 TB/s).
+// Tried and slower: ranges of 16384; a row's blocks of 64 logits dealt out among its workgroups, which spreads the frequent
+// low token numbers but takes twice the instructions per token (short histories 0.5 us faster, 32768 tokens 2 us slower).
+// Rows are the grid's fast axis: with a multiple of eight of them all ranges of a row run on one XCD, whose L2 then serves the
+// history.
 template <int kType, int kThreads, bool kWhole>
 __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) {
   constexpr int kRange = kThreads * 4 * kConQuads;
@@ -69,20 +74,35 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   const int b = blockIdx.x, tid = threadIdx.x, V = a.V;
   float *out = a.out + (long long)b * V;
   const int off = kWhole ? 0 : (int)(((uintptr_t)out >> 2) & 3);
-  const int lo = blockIdx.y * kRange - off;
   const char *row = (const char *)a.logits + (long long)b * a.row_stride * kValue;
   const bool quads = kWhole || (((uintptr_t)(row - off * kValue) & (4 * kValue - 1)) == 0 && V >= 8);
   const int first_quad = (4 - off) & 3, last_quad = ((V - 4 + off) & ~3) - off;   // whole quads of the row: the first and the last
+  const int lo = (int)blockIdx.y * kRange - off;
+  // first logit of the thread's quad k (-3 .. -1: a quad that begins ahead of the row; V and more: none)
+  auto place = [&](int k) { return lo + 4 * (tid + k * kThreads); };
   // ---- requests ----
   float x[kConQuads][4];
   if (quads) {
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) load_quad<kType>(row, min(max(lo + 4 * (tid + k * kThreads), first_quad), last_quad), x[k]);
+    for (int k = 0; k < kConQuads; ++k) load_quad<kType>(row, min(max(place(k), first_quad), last_quad), x[k]);
   } else {
 #pragma unroll
     for (int k = 0; k < kConQuads; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(lo + 4 * (tid + k * kThreads) + e, 0), V - 1));
+      for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(place(k) + e, 0), V - 1));
+  }
+  int n = 0, first = 0;
+  float rep = 1.f, pres = 0.f, freq = 0.f;
+  const int32_t *ids = a.tokens + (long long)b * a.token_stride;
+  const bool by_four = a.tokens && ((uintptr_t)ids & 15) == 0 && a.max_tokens >= 4;
+  int4 ahead = make_int4(0, 0, 0, 0);
+  if (by_four) ahead = ((const int4 *)ids)[min(tid, (a.max_tokens >> 2) - 1)];
+  if (a.tokens) {
+    n = a.lengths[b];
+    if (a.prompt_lengths) first = a.prompt_lengths[b];
+    if (a.repetition) rep = a.repetition[b];
+    if (a.presence) pres = a.presence[b];
+    if (a.frequency) freq = a.frequency[b];
   }
   typename std::conditional<kWhole, unsigned, unsigned long long>::type bits[kConQuads];   // the quad's mask bits, and what lies behind them
 #pragma unroll
@@ -95,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
 #pragma unroll
       for (int k = 0; k < kConQuads; ++k) {
         // (a quad that starts ahead of the row takes its bits from the row's first word, moved up)
-        const int i = lo + 4 * (tid + k * kThreads), w = min(max(i, 0) >> 5, words - 1);
+        const int i = place(k), w = min(max(i, 0) >> 5, words - 1);
         if constexpr (kWhole) {
           bits[k] = mask[w] >> (i & 31);
         } else {
@@ -105,10 +125,6 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
       }
     }
   }
-  const int32_t *ids = a.tokens + (long long)b * a.token_stride;
-  const bool by_four = a.tokens && ((uintptr_t)ids & 15) == 0 && a.max_tokens >= 4;
-  int4 ahead = make_int4(0, 0, 0, 0);
-  if (by_four) ahead = ((const int4 *)ids)[min(tid, (a.max_tokens >> 2) - 1)];
   int b0 = 0, b1 = 0, bias_ahead = -1;
   if (a.bias_offsets) {
     b0 = min(max(a.bias_offsets[b], 0), a.n_bias);
@@ -119,53 +135,55 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   if (!kWhole && quads) {
 #pragma unroll
     for (int k = 0; k < kConQuads; ++k) {
-      const int i = lo + 4 * (tid + k * kThreads);
+      const int i = place(k);
       if (i < 0 || (i + 4 > V && i < V)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(i + e, 0), V - 1));
       }
     }
   }
-  const int n = a.tokens ? min(max(a.lengths[b], 0), a.max_tokens) : 0;
-  // slot s of the LDS is token lo + s
-  auto in_range = [&](int id, unsigned &at) {
-    at = (unsigned)id - (unsigned)lo;
-    return (unsigned)id < (unsigned)V && at < (unsigned)kRange;
-  };
+  // Token id's slot is id - lo.  (An id of -3 .. -1 may find a slot ahead of the row: nothing reads it.)
+  const unsigned size = (unsigned)min(kRange, V - lo);
+  n = min(max(n, 0), a.max_tokens);
   // ---- the history's counts ----
   if (n > 0) {
-    const int first = a.prompt_lengths ? a.prompt_lengths[b] : 0;
-    const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f;
-    const float freq = a.frequency ? a.frequency[b] : 0.f;
 #pragma unroll
     for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
     __syncthreads();
-    auto count = [&](int id, int i) {
-      unsigned at;
-      if (in_range(id, at)) {
-        if (i < first) atomicOr(&slot[at], kConSeen);
+    // kind: 0 prompt, 1 generated, 2 either
+    auto count = [&](int id, int i, auto kind) {
+      const unsigned at = (unsigned)id - (unsigned)lo;
+      if (at < size) {
+        if (kind == 0 || (kind == 2 && i < first)) atomicOr(&slot[at], kConSeen);
         else atomicAdd(&slot[at], 1u);
       }
     };
-    auto count4 = [&](const int4 &v, int i) {
-      count(v.x, i);
-      count(v.y, i + 1);
-      count(v.z, i + 2);
-      count(v.w, i + 3);
+    auto count4 = [&](const int4 &v, int i, auto kind) {
+      count(v.x, i, kind);
+      count(v.y, i + 1, kind);
+      count(v.z, i + 2, kind);
+      count(v.w, i + 3, kind);
     };
     int done = 0;
     if (by_four) {
       const int groups = n >> 2;
-      if (tid < groups) count4(ahead, 4 * tid);
-      for (int g0 = tid + kThreads; g0 < groups; g0 += 4 * kThreads) {
-        int4 v[4];
+      // (a wavefront's 256 tokens are mostly of one kind)
+      auto count_group = [&](const int4 &v, int g) {
+        const int w0 = __builtin_amdgcn_readfirstlane(4 * g);
+        if (w0 >= first) count4(v, 4 * g, std::integral_constant<int, 1>{});
+        else if (w0 + 4 * kWave <= first) count4(v, 4 * g, std::integral_constant<int, 0>{});
+        else count4(v, 4 * g, std::integral_constant<int, 2>{});
+      };
+      if (tid < groups) count_group(ahead, tid);
+      for (int g0 = tid + kThreads; g0 < groups; g0 += kConAhead * kThreads) {
+        int4 v[kConAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = ((const int4 *)ids)[min(g0 + u * kThreads, groups - 1)];
+        for (int u = 0; u < kConAhead; ++u) v[u] = ((const int4 *)ids)[min(g0 + u * kThreads, groups - 1)];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kConAhead; ++u) {
           const int g = g0 + u * kThreads;
           if (g >= groups) break;
-          count4(v[u], 4 * g);
+          count_group(v[u], g);
         }
       }
       done = groups << 2;
@@ -176,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
       for (int u = 0; u < 8; ++u) v[u] = ids[min(i0 + u * kThreads, n - 1)];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (i0 + u * kThreads < n) count(v[u], i0 + u * kThreads);
+        if (i0 + u * kThreads < n) count(v[u], i0 + u * kThreads, std::integral_constant<int, 2>{});
     }
     __syncthreads();
 #pragma unroll
@@ -199,8 +217,8 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
     for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
     __syncthreads();
     for (int i = b0 + tid; i < b1; i += kThreads) {
-      unsigned at;
-      if (in_range(i == b0 + tid ? bias_ahead : a.bias_tokens[i], at)) atomicMax(&slot[at], (unsigned)(i - b0 + 1));
+      const unsigned at = (unsigned)(i == b0 + tid ? bias_ahead : a.bias_tokens[i]) - (unsigned)lo;
+      if (at < size) atomicMax(&slot[at], (unsigned)(i - b0 + 1));
     }
     __syncthreads();
 #pragma unroll
@@ -214,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   }
 #pragma unroll
   for (int k = 0; k < kConQuads; ++k) {
-    const int i = lo + 4 * (tid + k * kThreads);
+    const int i = place(k);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[k][e] = (bits[k] >> e) & 1u ? x[k][e] : -INFINITY;
     if (kWhole ? i < V : i >= 0 && i + 4 <= V) {
@@ -230,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
 hipError_t launch_constrain(const ConstrainLaunch &a, int type, hipStream_t stream) {
   const size_t value = type == kTypeFp32 ? 4 : 2;
   const bool whole = a.V % 4 == 0 && a.row_stride % 4 == 0 && (uintptr_t)a.logits % (4 * value) == 0 && (uintptr_t)a.out % 16 == 0;
-  const int threads = a.tokens && a.max_tokens >= 8192 ? 512 : 256;
+  const int threads = a.tokens && a.max_tokens >= 2048 ? 512 : 256;      // (see the kernel)
   const int range = threads * 4 * kConQuads;
   const dim3 grid(a.B, (a.V + 3 + range - 1) / range);     // (a row may start three places into its first quad)
 #define CONFKV_CASE(t, n) \
