@@ -179,7 +179,8 @@ typedef struct conf_kv_stats {
 /* Environment variables read once by conf_kv_create (test and measurement hooks; none is
  * needed in normal use): CONF_KV_SPLITS=n asks for n workgroups per unit in conf_kv_attend
  * instead of the planned number (clamped to what the unit's length allows);
- * CONF_KV_TWO_LAUNCH=1 forces the two-launch form of conf_kv_attend; CONF_KV_NO_MFMA=1 (read
+ * CONF_KV_TWO_LAUNCH=1 forces the two-launch form of conf_kv_attend; CONF_KV_SHARED_ROWS=1/2/4 the number of
+ * wavefronts side by side along the rows of conf_kv_attend_shared's prefix kernel; CONF_KV_NO_MFMA=1 (read
  * at the first plan of the process) keeps every shape on the vector-ALU streaming body;
  * CONF_KV_SPIN_LIMIT=n bounds the in-kernel waits for other workgroups to n polls (default
  * 400000, about 0.4 s; an expired wait ends the kernel early and counts a device error);

@@ -199,6 +199,7 @@ class ConfKV:
             raise RuntimeError("ConfKV needs a GPU: the decode path has no CPU implementation")
         self._torch = torch
         self._type = {torch.float32: TYPE_FP32, torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}
+        self._half, self._f32, self._i32 = torch.float16, torch.float32, torch.int32
         self._current_stream = _stream_getter(torch)
         self.lib = load_library()
         self.cfg, self._nt, self._nl = make_config(**kw)
@@ -206,7 +207,10 @@ class ConfKV:
         kb = self.lib.conf_kv_scratch_bytes(C.byref(self.cfg))
         if sb == 0:
             raise ConfKVError(ERR_BAD_SHAPE, "conf_kv_state_bytes")
+        c = self.cfg
+        self._batch, self._q_heads, self._kv_heads, self._head_dim, self._vocab = c.batch, c.n_q_heads, c.n_kv_heads, c.head_dim, c.vocab
         self.state = torch.empty(sb, dtype=torch.uint8, device="cuda")
+        self._device = self.state.get_device()
         self.scratch = torch.empty(kb, dtype=torch.uint8, device="cuda")
         h = _P()
         self._check(self.lib.conf_kv_create(C.byref(h), C.byref(self.cfg), self.state.data_ptr(),
@@ -253,24 +257,24 @@ class ConfKV:
         """q16 / out16 [B][tq][Hq][D], knew16 / vnew16 [B][tq][Hkv][D] as attend_chunk takes them, behind a prefix that the
         sequences share: shared_k / shared_v float16 [Hkv][T][D] (a view of a longer buffer will do), of which sequence b sees
         the first seen[b] tokens (int32 [B]; None: all)."""
-        c, half = self.cfg, self._torch.float16
-        H, D, tq = c.n_kv_heads, c.head_dim, int(q16.shape[1])
-        T = int(shared_k.shape[1])
-        for name, t in (("shared_k", shared_k), ("shared_v", shared_v)):
-            sh, st, sd = t.stride()
-            if t.dtype != half or t.shape != (H, T, D) or t.device != self.state.device or (t.numel() and (sd != 1 or (T > 1 and st != D))):
-                raise ValueError(f"{name}: float16 [{H}][{T}][{D}] with dense rows on {self.state.device} is wanted, got {t.dtype} "
-                                 f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
-        stride = shared_k.stride(0) if H > 1 else T * D
-        if H > 1 and shared_v.stride(0) != stride:
-            raise ValueError("shared_k and shared_v: kv-heads equally far apart are wanted")
-        rows, new = (c.batch, tq, c.n_q_heads, D), (c.batch, tq, H, D)
-        want = self._want
-        prefix = _PREFIX.pack(shared_k.data_ptr(), shared_v.data_ptr(), stride, T,
-                              want("seen", seen, self._torch.int32, (c.batch,)))
+        B, H, Hq, D, half, want = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._half, self._want
+        tq = q16.shape[1]
+        shape = shared_k.shape
+        T = shape[1]
+        apart, v_apart = shared_k.stride(), shared_v.stride()
+        if (shape != (H, T, D) or shared_k.dtype is not half or shared_k.get_device() != self._device or shared_v.shape != shape or
+                shared_v.dtype is not half or shared_v.get_device() != self._device or
+                T and (apart[2] != 1 or v_apart[2] != 1 or T > 1 and (apart[1] != D or v_apart[1] != D) or
+                       H > 1 and apart[0] != v_apart[0])):
+            raise ValueError(f"shared_k, shared_v: float16 [{H}][{T}][{D}] with dense rows and equal strides on {self.state.device} are "
+                             f"wanted, got {shared_k.dtype} {tuple(shape)} {apart} and {shared_v.dtype} {tuple(shared_v.shape)} "
+                             f"{v_apart} on {shared_k.device} and {shared_v.device}")
+        rows, new = (B, tq, Hq, D), (B, tq, H, D)
+        prefix = _PREFIX.pack(shared_k.data_ptr(), shared_v.data_ptr(), apart[0] if H > 1 else T * D, T,
+                              want("seen", seen, self._i32, (B,)))
         return self._check(self.lib.conf_kv_attend_shared(self.h, layer, tq, prefix, want("q16", q16, half, rows),
                                                           want("knew16", knew16, half, new), want("vnew16", vnew16, half, new),
-                                                          want("out16", out16, half, rows), self._stream()), "conf_kv_attend_shared")
+                                                          want("out16", out16, half, rows), self._current_stream()), "conf_kv_attend_shared")
 
     def observe(self, layer: int, first: int, q16, out16=None):
         """q16 / out16 [B][tq][Hq][D]: queries of the cached slots first .. first + tq - 1; out16 optional."""
@@ -304,27 +308,29 @@ class ConfKV:
     def evict_compact(self):
         return self._check(self.lib.conf_kv_evict_compact(self.h, self._stream()), "conf_kv_evict_compact")
 
-    def _want(self, name: str, t, dtype, shape=None):
+    # (Host time per call counts: an attribute of a tensor costs some 80 ns, its shape 160.  So every tensor is asked once, and
+    # what it lacks is only worked out for the message.)
+    def _want(self, name: str, t, dtype, shape):
         """The device pointer of a dense tensor that has to be as the call takes it (None: 0)."""
         if t is None:
             return 0
-        if t.dtype != dtype or (shape is not None and t.shape != shape) or not t.is_contiguous() or t.device != self.state.device:
-            raise ValueError(f"{name}: a contiguous {dtype} tensor{'' if shape is None else f' of shape {tuple(shape)}'} on "
-                             f"{self.state.device} is wanted, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-        return t.data_ptr()
+        if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == self._device:
+            return t.data_ptr()
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {self.state.device} is wanted, got "
+                         f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
 
-    def _rows(self, name: str, t, like, heads: int):
-        """Pointer and strides of q, k or v [B][T][heads][D] with dense heads, of the type and tokens of `like`."""
+    def _rows(self, name: str, t, dtype, tokens: int, heads: int):
+        """Pointer and strides of q, k or v [B][T][heads][D] with dense heads."""
         if t is None:
             return 0, 0, 0
-        c = self.cfg
-        if t.dtype != like.dtype or t.shape != (c.batch, like.shape[1], heads, c.head_dim) or t.device != self.state.device:
-            raise ValueError(f"{name}: {like.dtype} [{c.batch}][{like.shape[1]}][{heads}][{c.head_dim}] on {self.state.device} is "
-                             f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        sb, st, sh, sd = t.stride()
-        if t.numel() and (sd != 1 or (sh != c.head_dim and heads > 1)):
+        B, D = self._batch, self._head_dim
+        sb, st, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+        if t.dtype is not dtype or t.shape != (B, tokens, heads, D) or t.get_device() != self._device:
+            raise ValueError(f"{name}: {dtype} [{B}][{tokens}][{heads}][{D}] on {self.state.device} is wanted, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        if (sd != 1 or (sh != D and heads > 1)) and tokens:
             raise ValueError(f"{name}: the heads of a token are dense, got strides {t.stride()}")
-        return t.data_ptr(), sb if c.batch > 1 else 0, st if t.shape[1] > 1 else 0
+        return t.data_ptr(), sb if B > 1 else 0, st if tokens > 1 else 0      # (a size of 1 may come with any stride)
 
     def prepare_qkv(self, layer: int, q, k, v, q16=None, k16=None, v16=None, freq=None, pos=None, first: int = 0, q_weight=None,
                     k_weight=None, eps: float = 1e-6, interleaved: bool = False, prompt: bool = False):
@@ -334,22 +340,21 @@ class ConfKV:
         pos * freq, one rounding.  pos int32 [B][T], or None: the positions the next appended tokens of the layer get; `first` is
         added.  Each of q, k and v may be None together with its destination."""
         like = q if q is not None else k if k is not None else v
-        c = self.cfg
         if like is None or like.dim() != 4 or like.dtype not in self._type:
             raise ValueError("prepare_qkv: q, k or v [B][T][heads][D] of float32, float16 or bfloat16 is wanted")
-        B, T, H, D = c.batch, like.shape[1], c.n_kv_heads, c.head_dim
-        half = self._torch.float16
-        f32 = self._torch.float32
-        qp, qb, qt = self._rows("q", q, like, c.n_q_heads)
-        kp, kb, kt = self._rows("k", k, like, H)
-        vp, vb, vt = self._rows("v", v, like, H)
+        B, H, Hq, D, want = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._want
+        half, f32, dtype = self._half, self._f32, like.dtype
+        T = like.shape[1]
+        qp, qb, qt = self._rows("q", q, dtype, T, Hq)
+        kp, kb, kt = self._rows("k", k, dtype, T, H)
+        vp, vb, vt = self._rows("v", v, dtype, T, H)
         rows = (B, H, T, D) if prompt else (B, T, H, D)
-        args = _QKV.pack(T, self._type[like.dtype], qp, kp, vp, qb, qt, kb, kt, vb, vt, self._want("q_weight", q_weight, f32, (D,)),
-                         self._want("k_weight", k_weight, f32, (D,)), self._want("freq", freq, f32),
-                         self._want("pos", pos, self._torch.int32, (B, T)), first, 0 if freq is None else 2 * freq.numel(),
-                         bool(interleaved), bool(prompt), eps, self._want("q16", q16, half, (B, T, c.n_q_heads, D)),
-                         self._want("k16", k16, half, rows), self._want("v16", v16, half, rows))
-        return self._check(self.lib.conf_kv_prepare_qkv(self.h, layer, args, self._stream()), "conf_kv_prepare_qkv")
+        pairs = 0 if freq is None else freq.numel()
+        args = _QKV.pack(T, self._type[dtype], qp, kp, vp, qb, qt, kb, kt, vb, vt, want("q_weight", q_weight, f32, (D,)),
+                         want("k_weight", k_weight, f32, (D,)), want("freq", freq, f32, (pairs,)),
+                         want("pos", pos, self._i32, (B, T)), first, 2 * pairs, 1 if interleaved else 0, 1 if prompt else 0, eps,
+                         want("q16", q16, half, (B, T, Hq, D)), want("k16", k16, half, rows), want("v16", v16, half, rows))
+        return self._check(self.lib.conf_kv_prepare_qkv(self.h, layer, args, self._current_stream()), "conf_kv_prepare_qkv")
 
     def constrain(self, logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
                   frequency=None, bias_offsets=None, bias_tokens=None, bias_values=None, allowed=None, allowed_rows=None):
@@ -357,32 +362,36 @@ class ConfKV:
         tokens int32 [B][n] with lengths and prompt_lengths int32 [B]; repetition, presence, frequency float32 [B]; biases as
         bias_offsets int32 [B + 1] into bias_tokens int32 and bias_values float32; allowed int32 (or uint32) [masks][ceil(V / 32)]
         with allowed_rows int32 [B] or one mask row per sequence."""
-        c, torch = self.cfg, self._torch
-        B, V, want, i32, f32 = c.batch, c.vocab, self._want, torch.int32, torch.float32
-        if logits.dtype not in self._type or logits.shape != (B, V) or logits.device != self.state.device or logits.stride(1) != 1:
+        B, V, want, i32, f32, device = self._batch, self._vocab, self._want, self._i32, self._f32, self._device
+        row = (B,)
+        kind = self._type.get(logits.dtype)
+        apart, step = logits.stride() if logits.dim() == 2 else (0, 0)
+        if kind is None or logits.shape != (B, V) or logits.get_device() != device or step != 1:
             raise ValueError(f"logits: [{B}][{V}] of float32, float16 or bfloat16 with dense rows is wanted, got {logits.dtype} "
                              f"{tuple(logits.shape)} strides {logits.stride()} on {logits.device}")
-        n = 0
+        n = ids = ids_apart = m = masks = 0
         if tokens is not None:
             n = tokens.shape[1] if tokens.dim() == 2 else -1
-            if tokens.dtype != i32 or tokens.shape != (B, n) or tokens.device != self.state.device or (n > 1 and tokens.stride(1) != 1):
+            if tokens.dtype is not i32 or tokens.shape != (B, n) or tokens.get_device() != device or (n > 1 and tokens.stride()[1] != 1):
                 raise ValueError(f"tokens: int32 [{B}][n] with dense rows is wanted, got {tokens.dtype} {tuple(tokens.shape)}")
+            if n:
+                ids, ids_apart = tokens.data_ptr(), tokens.stride()[0] if B > 1 else n
         elif repetition is not None or presence is not None or frequency is not None:
             raise ValueError("tokens: penalties need the history")
-        m = 0 if bias_tokens is None else bias_tokens.numel()
-        masks = 0 if allowed is None else allowed.shape[0]
-        if allowed is not None and allowed.dtype != i32:
-            allowed = allowed.view(i32)
-        row = (B,)
+        if bias_tokens is not None:
+            m = bias_tokens.numel()
+        if allowed is not None:
+            masks = allowed.shape[0]
+            if allowed.dtype is not i32:
+                allowed = allowed.view(i32)
         args = _CONSTRAINTS.pack(
-            self._type[logits.dtype], n, logits.data_ptr(), logits.stride(0) if B > 1 else V, want("out", out, f32, (B, V)),
-            0 if tokens is None else tokens.data_ptr(), (tokens.stride(0) if B > 1 else n) if n else 0,
+            kind, n, logits.data_ptr(), apart if B > 1 else V, want("out", out, f32, (B, V)), ids, ids_apart,
             want("lengths", lengths, i32, row), want("prompt_lengths", prompt_lengths, i32, row),
             want("repetition", repetition, f32, row), want("presence", presence, f32, row), want("frequency", frequency, f32, row),
             want("bias_offsets", bias_offsets, i32, (B + 1,)), want("bias_tokens", bias_tokens, i32, (m,)),
             want("bias_values", bias_values, f32, (m,)), m, masks, want("allowed", allowed, i32, (masks, (V + 31) // 32)),
             want("allowed_rows", allowed_rows, i32, row))
-        return self._check(self.lib.conf_kv_constrain(self.h, args, self._stream()), "conf_kv_constrain")
+        return self._check(self.lib.conf_kv_constrain(self.h, args, self._current_stream()), "conf_kv_constrain")
 
     def lengths(self):
         c = self.cfg

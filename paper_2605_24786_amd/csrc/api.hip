@@ -181,6 +181,7 @@ struct conf_kv_handle {
   bool static_plan = false;          // conf_kv_static_plan: launch shapes from the budgets, not the lengths so far
   int forced_splits = 0;            // CONF_KV_SPLITS at create (tests, sweeps)
   bool force_two_launch = false;    // CONF_KV_TWO_LAUNCH at create (tests)
+  int forced_row_waves = 0;         // CONF_KV_SHARED_ROWS at create (tests, sweeps)
   int withhold = 0;                 // CONF_KV_TEST_WITHHOLD at create (tests of the expiry path)
   int kv_major = 0;                 // splits of a unit on one XCD (eight kv-heads or a multiple; CONF_KV_GRID_KV_MAJOR overrides)
   bool evict_separate = false;      // CONF_KV_EVICT_ONE=0 at create (tests)
@@ -236,6 +237,7 @@ int conf_kv_create(conf_kv_handle **out, const conf_kv_config *cfg, void *dev_st
   h->fresh_len.assign(L, -1);
   if (const char *fs = getenv("CONF_KV_SPLITS")) h->forced_splits = atoi(fs);
   if (const char *tl = getenv("CONF_KV_TWO_LAUNCH")) h->force_two_launch = atoi(tl) != 0;
+  if (const char *sr = getenv("CONF_KV_SHARED_ROWS")) h->forced_row_waves = atoi(sr);
   if (const char *eo = getenv("CONF_KV_EVICT_ONE")) h->evict_separate = atoi(eo) == 0;
   if (const char *wh = getenv("CONF_KV_TEST_WITHHOLD")) h->withhold = atoi(wh) != 0;
   h->kv_major = cfg->n_kv_heads % 8 == 0;
@@ -471,7 +473,7 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
   if (shared) {
     SharedLaunch p{};
     SharedPlan sp;
-    shared_plan(h->cfg.batch * tq * h->cv.G, h->cfg.n_kv_heads, prefix->tokens, device_cu_count(), &sp);
+    shared_plan(h->cfg.batch * tq * h->cv.G, h->cfg.n_kv_heads, h->cfg.head_dim, prefix->tokens, device_cu_count(), h->forced_row_waves, &sp);
     p.k = (const __half *)prefix->dev_k16;
     p.v = (const __half *)prefix->dev_v16;
     p.head_stride = prefix->head_stride;

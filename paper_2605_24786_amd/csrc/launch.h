@@ -132,7 +132,7 @@ hipError_t launch_attend(const CacheView &cv, const AttendLaunch &a, const Atten
 // ---- attend_shared.hip ----
 constexpr int kSharedMaxParts = 64;
 struct SharedPlan {
-  int row_waves;           // wavefronts of a workgroup side by side along the rows
+  int row_waves;           // wavefronts of a workgroup side by side along the rows: 1, 2 or 4
   int blocks;              // workgroups along the rows of a kv-head
   int parts, part_keys;    // parts of the prefix and the keys of one
 };
@@ -147,7 +147,8 @@ struct SharedLaunch {
   float sm_scale;
 };
 size_t shared_parts_most(int tokens);      // parts a prefix of up to that many tokens can be cut into
-void shared_plan(int rows, int Hkv, int T, int cus, SharedPlan *plan);
+// rows of a kv-head; forced_row_waves: 1, 2 or 4, else the plan's own choice
+void shared_plan(int rows, int Hkv, int D, int T, int cus, int forced_row_waves, SharedPlan *plan);
 int device_cu_count();
 hipError_t launch_shared_prefix(const SharedLaunch &a, const SharedPlan &p, int D, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,

@@ -51,9 +51,10 @@ class _Case:
     """A handle of one layer, its oracle units and the prefix."""
 
     def __init__(self, lib, torch, monkeypatch, D, G, H, B, T, T0, W, tq=1, splits=0, two_launch=False, scales="token",
-                 layout="contiguous", seen=None, seed=0, budget=None, spread=1.0):
+                 layout="contiguous", seen=None, seed=0, budget=None, spread=1.0, row_waves=0):
         monkeypatch.setenv("CONF_KV_SPLITS", str(splits))
         monkeypatch.setenv("CONF_KV_TWO_LAUNCH", str(int(two_launch)))
+        monkeypatch.setenv("CONF_KV_SHARED_ROWS", str(row_waves))
         self.torch, self.D, self.G, self.H, self.B, self.T, self.W, self.tq = torch, D, G, H, B, T, W, tq
         self.budget = budget or T0 + 40
         page = 16 if layout == "paged" else 0
@@ -142,14 +143,17 @@ _SHAPES = [
     (128, 5, 1, 2, 160, 120, -1, 3, 0),
     (128, 8, 1, 5, 2000, 64, 8, 2, 1),
     (128, 4, 1, 1, 9000, 300, 40, 1, 2),       # more parts than wavefronts
+    (64, 8, 24, 5, 5003, 60, 16, 1, 0),        # several turns of a workgroup
+    (128, 4, 32, 9, 1801, 40, 16, 1, 0),
 ]
 
 
 @pytest.mark.parametrize("D,G,H,B,T,T0,W,tq,splits", _SHAPES)
-@pytest.mark.parametrize("two_launch", [False, True])
-def test_outputs_and_importance(lib, torch_cuda, monkeypatch, D, G, H, B, T, T0, W, tq, splits, two_launch):
-    print(f"shared D={D} G={G} H={H} B={B} T={T} T0={T0} W={W} tq={tq} splits={splits} two_launch={two_launch}", flush=True)
-    c = _Case(lib, torch_cuda, monkeypatch, D, G, H, B, T, T0, W, tq=tq, splits=splits, two_launch=two_launch, seed=T + B)
+@pytest.mark.parametrize("two_launch,row_waves", [(False, 1), (False, 2), (False, 4), (True, 0)])
+def test_outputs_and_importance(lib, torch_cuda, monkeypatch, D, G, H, B, T, T0, W, tq, splits, two_launch, row_waves):
+    print(f"shared D={D} G={G} H={H} B={B} T={T} T0={T0} W={W} tq={tq} splits={splits} two_launch={two_launch} rows {row_waves}", flush=True)
+    c = _Case(lib, torch_cuda, monkeypatch, D, G, H, B, T, T0, W, tq=tq, splits=splits, two_launch=two_launch, seed=T + B,
+              row_waves=row_waves)
     for t in range(2):
         worst = c.step(f"step {t}")
     print(f"  out {worst:.3g} x tolerance", flush=True)
@@ -165,11 +169,12 @@ def test_storage_variants(lib, torch_cuda, monkeypatch, G, scales, layout, W):
     c.close()
 
 
-@pytest.mark.parametrize("G,B,T", [(4, 7, 400), (1, 33, 300), (8, 20, 130)])
-def test_sequences_that_see_part_of_the_prefix(lib, torch_cuda, monkeypatch, G, B, T):
+@pytest.mark.parametrize("row_waves", [1, 2, 4])
+@pytest.mark.parametrize("G,B,T", [(4, 7, 400), (1, 33, 300), (8, 20, 130), (4, 40, 1500)])
+def test_sequences_that_see_part_of_the_prefix(lib, torch_cuda, monkeypatch, G, B, T, row_waves):
     """All of it, some, none; counts outside 0 .. T are held within."""
     seen = [(T, T // 2 + 1, 0, -7, T - 1, 2 ** 31 - 1, 1)[b % 7] for b in range(B)]
-    c = _Case(lib, torch_cuda, monkeypatch, 128, G, 1, B, T, 70, 16, seen=seen, seed=B)
+    c = _Case(lib, torch_cuda, monkeypatch, 128, G, 1, B, T, 70, 16, seen=seen, seed=B, row_waves=row_waves)
     c.step("part")
     c.seen = [0] * B
     c.step("nobody sees it")
@@ -204,15 +209,16 @@ def test_sharp_scores(lib, torch_cuda, monkeypatch):
         c.close()
 
 
+@pytest.mark.parametrize("row_waves", [1, 2, 4])
 @pytest.mark.parametrize("kind", ["inf value", "nan value", "nan key", "inf key"])
-def test_odd_values_reach_only_those_who_see_them(lib, torch_cuda, monkeypatch, kind):
+def test_odd_values_reach_only_those_who_see_them(lib, torch_cuda, monkeypatch, kind, row_waves):
     """A value or key that is no number shows in the sequences that see its token and in no other, also where their rows share
     tiles with rows that do see it."""
     torch = torch_cuda
     G, B, T, T0, D = 4, 9, 200, 50, 128
     at = 150
     seen = [T, at, at + 1, 0, 10, T, at, 100, 151]
-    c = _Case(lib, torch, monkeypatch, D, G, 1, B, T, T0, 16, seen=seen, seed=3)
+    c = _Case(lib, torch, monkeypatch, D, G, 1, B, T, T0, 16, seen=seen, seed=3, row_waves=row_waves)
     plane = c.shared[1] if "value" in kind else c.shared[0]
     plane[0, at, 3] = math.nan if "nan" in kind else math.inf
     q, kn, vn = c.inputs()
