@@ -111,7 +111,7 @@ typedef struct conf_kv_config {
                                 the appended tokens                                            */
   int32_t layout;            /* conf_kv_layout: where the INT8 slots of a unit live              */
   int32_t max_shared;        /* most tokens of a shared prefix that conf_kv_attend_shared may be given (sizes the scratch
-                                buffer: up to 64 partial results per query row); 0: no such calls */
+                                buffer: up to 64 partial results per query row), up to 2^30; 0: none         */
 } conf_kv_config;
 
 typedef enum conf_kv_layout {
@@ -242,7 +242,7 @@ int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16,
  *      (so sum_i A_i = G), then ema_i <- lambda * ema_i + (1 - lambda) * A_i.
  * dev_q16: fp16 [B][Hq][D]; dev_knew16 / dev_vnew16: fp16 [B][Hkv][D]; dev_out16: fp16
  * [B][Hq][D], written.  All 16-byte aligned.
- * Exactly one conf_kv_attend per layer between two conf_kv_evict_compact calls
+ * Exactly one conf_kv_attend (conf_kv_attend_chunk, conf_kv_attend_shared) per layer between two conf_kv_evict_compact calls
  * (CONF_KV_ERR_BAD_STATE otherwise); CONF_KV_ERR_CAPACITY, before anything is launched,
  * if the unit could already hold `capacity` tokens.
  * The workgroups that share a unit exchange partial results inside the launch, so the launch
@@ -250,7 +250,7 @@ int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16,
  * running at the same time, only delay it (its waits are bounded at several hundred
  * milliseconds); a wait that does expire leaves the call's outputs undefined and is reported by
  * conf_kv_counters (device_errors, CONF_KV_ERR_DEVICE).  Two launches of this kind on two streams
- * (other handles: conf_kv_attend, conf_kv_attend_chunk, conf_kv_observe, conf_kv_step) may each
+ * (other handles: conf_kv_attend, conf_kv_attend_chunk, conf_kv_attend_shared, conf_kv_observe, conf_kv_step) may each
  * hold compute units that the other's workgroups wait for if together they need more than the
  * device has; order such calls by events where their grids are large.  A call of this function
  * takes up to one workgroup per compute unit.  Calls of more than 16 / G tokens

@@ -58,7 +58,7 @@ bool config_ok(const conf_kv_config *c) {
   if (c->rank_scope != CONF_KV_SCOPE_KV_HEAD && c->rank_scope != CONF_KV_SCOPE_LAYER) return false;
   if (c->scale_mode != CONF_KV_SCALES_TOKEN && c->scale_mode != CONF_KV_SCALES_CHANNEL) return false;
   if (c->scale_mode == CONF_KV_SCALES_CHANNEL && (c->head_dim != 128 || c->fp16_window < 0)) return false;
-  if (c->max_chunk < 0 || c->max_shared < 0) return false;
+  if (c->max_chunk < 0 || c->max_shared < 0 || c->max_shared > 1 << 30) return false;
   // multi-token calls: one tile of 16 query rows per unit, or up to kWideRowsMax rows on the
   // many-rows kernel (per-token scales only)
   if (c->max_chunk > 1) {
@@ -592,6 +592,7 @@ int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *arg
   if (T < 0 || (long long)B * T > (1ll << 30) || q.type < CONF_KV_TYPE_FP32 || q.type > CONF_KV_TYPE_BF16)
     return CONF_KV_ERR_INVALID_ARG;
   if (q.rotated < 0 || q.rotated > D || q.rotated % 16 || (q.rotated > 0 && !q.dev_freq)) return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)q.dev_q_weight | (uintptr_t)q.dev_k_weight | (uintptr_t)q.dev_freq | (uintptr_t)q.dev_pos) & 3) return CONF_KV_ERR_INVALID_ARG;
   if ((q.dev_q_weight || q.dev_k_weight) && !(q.eps >= 0.f && q.eps <= 3.0e38f)) return CONF_KV_ERR_INVALID_ARG;
   if (T == 0) return CONF_KV_OK;
   struct Part { const void *src; void *dst; int heads; int64_t batch, token; };
@@ -659,6 +660,10 @@ int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_k
   if ((uintptr_t)c.dev_logits % vb || (uintptr_t)c.dev_out % 4) return CONF_KV_ERR_INVALID_ARG;
   const bool in_place = c.dev_logits == c.dev_out && c.type == CONF_KV_TYPE_FP32 && c.logits_stride == V;
   if (!in_place && overlap(c.dev_logits, ((B - 1) * (size_t)c.logits_stride + V) * vb, c.dev_out, (size_t)B * V * 4))
+    return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)c.dev_tokens | (uintptr_t)c.dev_lengths | (uintptr_t)c.dev_prompt_lengths | (uintptr_t)c.dev_repetition |
+       (uintptr_t)c.dev_presence | (uintptr_t)c.dev_frequency | (uintptr_t)c.dev_bias_offsets | (uintptr_t)c.dev_bias_tokens |
+       (uintptr_t)c.dev_bias_values | (uintptr_t)c.dev_allowed | (uintptr_t)c.dev_allowed_rows) & 3)
     return CONF_KV_ERR_INVALID_ARG;
   const bool penalties = c.dev_repetition || c.dev_presence || c.dev_frequency;
   if (V > 1 << 27) return CONF_KV_ERR_BAD_SHAPE;

@@ -5,10 +5,15 @@
 //   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position * freq[p]   for the pairs p of the first `rotated`
 //   channels: (y_p, y_(p + rotated/2)), or (y_2p, y_(2p+1)) when interleaved; the channels behind them stay y.
 //
-// A wavefront takes one token.  A row (one head of one token) is D / 16 lanes of sixteen channels, arranged as two runs of
-// eight such that a lane holds both halves of its eight pairs: no exchange between lanes but the sum of squares.  The angle
-// of pair `lane` is computed once per token by that lane, the product in float64 (at position 10^6 a float32 angle is off by
-// 0.03) and reduced to turns there, and shared through LDS.
+// A wavefront takes one token.  A row (one head of one token) is D / 16 lanes of sixteen channels, in runs of sixteen bytes as
+// stored, arranged such that lanes side by side load neighbouring runs and a lane holds both halves of its pairs: no exchange
+// between lanes but the sum of squares.  The angle of pair `lane` is computed once per token by that lane, the product in
+// float64 (at position 10^6 a float32 angle is off by 0.03) and reduced to turns there, and shared through LDS.
+// What bounds it: bytes.  Where every access of a wavefront is whole 128-byte lines (128 channels of 16 bits, none or all of
+// which turn, or interleaved) streaming accesses take eight prompts of 4096 tokens, 48 heads, BF16 from 152 to 141 us (5.7 TB/s read
+// and written, more than a large copy reaches); where a line is met by two accesses they cost (64 channels of float32, 32 of
+// them turning, 5271 tokens: 162 and 200 us), so these, and short calls, whose result is read next, do without.
+// A decode step's call is a launch (3 to 4 us on the device): its rows are spread over as many wavefronts as they make.
 #include "confkv_dev.h"
 #include "launch.h"
 
@@ -16,51 +21,54 @@ namespace confkv {
 
 constexpr int kPrepWaves = 4;
 
-typedef float prep_f8 __attribute__((ext_vector_type(8)));
+typedef _Float16 prep_h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 prep_h8 __attribute__((ext_vector_type(8)));
 
-// eight neighbouring values as stored, and as float32
-template <int kType> struct Run8 { int4 a; };
-template <> struct Run8<kTypeFp32> { int4 a, b; };
-
-template <int kType>
-__device__ __forceinline__ Run8<kType> load_run(const void *base, long long at) {
-  Run8<kType> r;
+// Sixteen bytes of values as float32: eight, or four of a float32 source.
+template <int kType, bool kStream>
+__device__ __forceinline__ void load_run(const void *base, long long at, int4 &raw) {
   const char *p = (const char *)base + at * (kType == kTypeFp32 ? 4 : 2);
-  r.a = ld_stream16(p);
-  if constexpr (kType == kTypeFp32) r.b = ld_stream16(p + 16);
-  return r;
+  raw = kStream ? ld_stream16(p) : *(const int4 *)p;
 }
-template <int kType>
-__device__ __forceinline__ void unpack_run(const Run8<kType> &r, float (&f)[16], int at) {
+template <int kType, int kRun>
+__device__ __forceinline__ void unpack_run(const int4 &r, float (&f)[kRun]) {
+  const unsigned v[4] = {(unsigned)r.x, (unsigned)r.y, (unsigned)r.z, (unsigned)r.w};
   if constexpr (kType == kTypeFp32) {
-    const int v[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[at + e] = __int_as_float(v[e]);
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
   } else if constexpr (kType == kTypeFp16) {
-    const prep_h8 h = __builtin_bit_cast(prep_h8, r.a);
+    const prep_h8 h = __builtin_bit_cast(prep_h8, r);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[at + e] = (float)h[e];
+    for (int e = 0; e < 8; ++e) f[e] = (float)h[e];
   } else {
-    const unsigned v[4] = {(unsigned)r.a.x, (unsigned)r.a.y, (unsigned)r.a.z, (unsigned)r.a.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      f[at + 2 * e] = __uint_as_float(v[e] << 16);
-      f[at + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+      f[2 * e] = __uint_as_float(v[e] << 16);
+      f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
     }
   }
 }
-__device__ __forceinline__ void store_run(__half *dst, const float (&f)[16], int at) {
-  prep_h8 h;
+template <int kRun, bool kStream>
+__device__ __forceinline__ void store_run(__half *dst, const float (&f)[kRun]) {
+  if constexpr (kRun == 8) {
+    prep_h8 h;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) h[e] = (_Float16)f[at + e];
-  *(int4 *)dst = __builtin_bit_cast(int4, h);
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)f[e];
+    if constexpr (kStream) st_stream16(dst, __builtin_bit_cast(int4, h));
+    else *(int4 *)dst = __builtin_bit_cast(int4, h);
+  } else {
+    prep_h4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = (_Float16)f[e];
+    *(int2 *)dst = __builtin_bit_cast(int2, h);
+  }
 }
 
 // Rows of a token in the order q, k, v, in passes of 64 / (D / 16) rows of one kind each; `per` passes per wavefront.
-template <int kType, int D>
+template <int kType, int D, bool kStream>
 __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaunch a, int parts, int per) {
   constexpr int LPR = D / 16, RPP = kWave / LPR;
+  constexpr int kRun = kType == kTypeFp32 ? 4 : 8, kSets = 8 / kRun;   // a lane's sets of two runs
   __shared__ float2 s_turn[kPrepWaves][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long task = (long long)blockIdx.x * kPrepWaves + w;
@@ -73,9 +81,6 @@ __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaun
   const int p0 = part * per, p1 = min(p0 + per, nq + nk + nv);
   const int c = lane % LPR, r = lane / LPR;
   const int half = a.rotated >> 1;
-  const bool turns = a.interleaved ? 16 * c < a.rotated : 8 * c < half;
-  // channels of the lane's two runs
-  const int oa = turns && !a.interleaved ? 8 * c : 16 * c, ob = turns && !a.interleaved ? half + 8 * c : 16 * c + 8;
   if (p0 < nq + nk) {
     if (lane < half) {
       const long long pos = a.pos ? (long long)a.pos[tok] : (long long)*a.next + t;
@@ -87,12 +92,35 @@ __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaun
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  float cs[8], sn[8];
+  // Set s of the lane: the runs at channels at[s][0] and at[s][1], and cosine and sine of their kRun pairs.  With j = kRun (c + LPR s):
+  //   halves:       (j, j + rotated / 2) while j is below rotated / 2, else two runs of the channels that do not turn
+  //   interleaved:  (j, j + D / 2), each of which holds kRun / 2 pairs if it turns
+  int at[kSets][2];
+  bool turns[kSets][2];
+  float cs[kSets][kRun], sn[kSets][kRun];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 v = turns ? s_turn[w][8 * c + e] : make_float2(1.f, 0.f);
-    cs[e] = v.x;
-    sn[e] = v.y;
+  for (int s = 0; s < kSets; ++s) {
+    const int j = kRun * (c + LPR * s);
+    if (a.interleaved) {
+      at[s][0] = j;
+      at[s][1] = j + D / 2;
+    } else if (j < half) {
+      at[s][0] = j;
+      at[s][1] = j + half;
+    } else {
+      at[s][0] = half + j;
+      at[s][1] = half + j + (D - a.rotated) / 2;
+    }
+    turns[s][0] = at[s][0] < a.rotated;
+    turns[s][1] = at[s][1] < a.rotated;
+#pragma unroll
+    for (int e = 0; e < kRun; ++e) {
+      const int which = a.interleaved && e >= kRun / 2 ? 1 : 0;
+      const int pair = a.interleaved ? at[s][which] / 2 + (e & (kRun / 2 - 1)) : j + e;
+      const float2 v = turns[s][which] ? s_turn[w][pair] : make_float2(1.f, 0.f);
+      cs[s][e] = v.x;
+      sn[s][e] = v.y;
+    }
   }
   for (int p = p0; p < p1; ++p) {
     const int kind = p < nq ? 0 : p < nq + nk ? 1 : 2;
@@ -102,42 +130,64 @@ __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaun
     const void *src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
     const long long row = (kind == 0 ? b * a.q_batch + t * a.q_token
                                      : kind == 1 ? b * a.k_batch + t * a.k_token : b * a.v_batch + t * a.v_token) + head * D;
-    const int xa = kind == 2 ? 16 * c : oa, xb = kind == 2 ? 16 * c + 8 : ob;
-    float f[16];
-    unpack_run<kType>(load_run<kType>(src, row + xa), f, 0);
-    unpack_run<kType>(load_run<kType>(src, row + xb), f, 8);
+    int4 raw[kSets][2];
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) load_run<kType, kStream>(src, row + at[s][i], raw[s][i]);
+    float f[kSets][2][kRun];
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) unpack_run<kType, kRun>(raw[s][i], f[s][i]);
     const float *wt = kind == 0 ? a.wq : kind == 1 ? a.wk : nullptr;
     if (wt) {
       float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) ss = fmaf(f[e], f[e], ss);
+      for (int s = 0; s < kSets; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) ss = fmaf(f[s][i][e], f[s][i][e], ss);
 #pragma unroll
       for (int m = LPR / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, kWave);
       const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) f[e] *= inv * wt[e < 8 ? xa + e : xb + e - 8];
+      for (int s = 0; s < kSets; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) f[s][i][e] *= inv * wt[at[s][i] + e];
     }
-    if (kind < 2 && turns) {
-      if (a.interleaved) {
+    if (kind < 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = f[2 * e], y = f[2 * e + 1];
-          f[2 * e] = x * cs[e] - y * sn[e];
-          f[2 * e + 1] = y * cs[e] + x * sn[e];
-        }
-      } else {
+      for (int s = 0; s < kSets; ++s) {
+        if (a.interleaved) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = f[e], y = f[8 + e];
-          f[e] = x * cs[e] - y * sn[e];
-          f[8 + e] = y * cs[e] + x * sn[e];
+          for (int e = 0; e < kRun; ++e) {
+            const int i = e / (kRun / 2), o = 2 * (e & (kRun / 2 - 1));
+            if (turns[s][i]) {
+              const float x = f[s][i][o], y = f[s][i][o + 1];
+              f[s][i][o] = x * cs[s][e] - y * sn[s][e];
+              f[s][i][o + 1] = y * cs[s][e] + x * sn[s][e];
+            }
+          }
+        } else if (turns[s][0]) {
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) {
+            const float x = f[s][0][e], y = f[s][1][e];
+            f[s][0][e] = x * cs[s][e] - y * sn[s][e];
+            f[s][1][e] = y * cs[s][e] + x * sn[s][e];
+          }
         }
       }
     }
     __half *dst = kind == 0 ? a.q16 : kind == 1 ? a.k16 : a.v16;
     dst += (kind != 0 && a.prompt ? ((long long)b * a.Hkv + head) * a.tokens + t : tok * heads + head) * D;
-    store_run(dst + xa, f, 0);
-    store_run(dst + xb, f, 8);
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) store_run<kRun, kStream>(dst + at[s][i], f[s][i]);
   }
 }
 
@@ -151,9 +201,11 @@ hipError_t launch_prepare(const PrepareLaunch &a, int D, int type, hipStream_t s
   const int parts = (passes + per - 1) / per;
   const long long blocks = (tokens * parts + kPrepWaves - 1) / kPrepWaves;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  auto fn = type == kTypeFp32 ? (D == 64 ? prepare_kernel<kTypeFp32, 64> : prepare_kernel<kTypeFp32, 128>)
-          : type == kTypeFp16 ? (D == 64 ? prepare_kernel<kTypeFp16, 64> : prepare_kernel<kTypeFp16, 128>)
-                              : (D == 64 ? prepare_kernel<kTypeBf16, 64> : prepare_kernel<kTypeBf16, 128>);
+  // (see the top)
+  const bool stream_lines = D == 128 && type != kTypeFp32 && (a.interleaved || a.rotated == 0 || a.rotated == D) && tokens >= 4096;
+  auto fn = type == kTypeFp32 ? (D == 64 ? prepare_kernel<kTypeFp32, 64, false> : prepare_kernel<kTypeFp32, 128, false>)
+          : type == kTypeFp16 ? (D == 64 ? prepare_kernel<kTypeFp16, 64, false> : stream_lines ? prepare_kernel<kTypeFp16, 128, true> : prepare_kernel<kTypeFp16, 128, false>)
+                              : (D == 64 ? prepare_kernel<kTypeBf16, 64, false> : stream_lines ? prepare_kernel<kTypeBf16, 128, true> : prepare_kernel<kTypeBf16, 128, false>);
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(kPrepWaves * kWave), 0, stream, a, parts, per);
   return hipGetLastError();
 }

@@ -85,6 +85,8 @@ def _run(torch, lib, B, T, Hq, Hkv, D, dtype, rotated, interleaved, prompt, norm
     (2, 3, 8, 8, 128, 0, False, True, "both"),          # nothing turns
     (2, 3, 8, 8, 128, 16, True, False, None),
     (1, 4099, 4, 2, 64, 32, False, True, "both"),       # enough wavefronts for one per token
+    (2, 2050, 4, 2, 128, 128, False, True, "both"),     # streaming accesses of whole lines
+    (3, 1400, 9, 3, 128, 64, True, False, "q"),
 ])
 def test_rows_match_the_formulas(lib, torch_cuda, dtype, B, T, Hq, Hkv, D, rotated, interleaved, prompt, norm):
     torch = torch_cuda
