@@ -8,6 +8,7 @@
 // A workgroup owns a range of the vocabulary of one row: it requests its logits and mask words, reads the row's whole history
 // meanwhile and counts the tokens of its own range in LDS (integer atomics, so that the order of arrival changes nothing),
 // applies the counts, reuses the LDS for the places of the biases, and writes its range once.
+#include <algorithm>
 #include <type_traits>
 
 #include "confkv_dev.h"
@@ -15,7 +16,7 @@
 
 namespace confkv {
 
-constexpr int kConQuads = 4;                          // groups of four logits per thread
+constexpr int kConThreads = 1024;
 constexpr int kConAhead = 4;                          // groups of four tokens per thread in flight
 constexpr unsigned kConSeen = 0x80000000u;            // the token occurs in the history; the other bits count its generated part
 
@@ -57,17 +58,19 @@ __device__ __forceinline__ void load_quad(const void *row, int i, float (&x)[4])
 // What bounds it: a call on a few rows is a chain -- arguments, lengths, the history, two barriers, the result -- so whatever can
 // be requested ahead of what it waits for is (first tokens of the history ahead of its length, biases ahead of the counts).  On
 // many rows it is the bytes of the logits and, with long histories, the vector ALU: every range passes over the row's whole
-// history, some seven instructions per token and wavefront.  So ranges of 4096 logits for short histories and of 8192 (half the
-// passes, half the workgroups) from 2048 tokens on.
-// us with 4096 and 8192 (BF16 logits, 64 biases, a mask): 1 row of 128256 and 300 tokens 4.9, 5.0, 4096 tokens 6.2, 5.9, 32768
-// 10.8, 8.1; 8 rows and 4096 tokens 6.4, 6.4; 32 rows and 300 tokens 8.4, 8.9, 32768 16.8, 13.7, no history 7.1, 7.4 (25 MB: 3.5 TB/s).
-// Tried and slower: ranges of 16384; a row's blocks of 64 logits dealt out among its workgroups, which spreads the frequent
-// low token numbers but takes twice the instructions per token (short histories 0.5 us faster, 32768 tokens 2 us slower).
+// history, some seven instructions per token and wavefront.  So sixteen wavefronts share a pass, and a range is 4096 logits per
+// quad of a thread, with as many quads (1, 2, 4 or 5) as make the fewest rounds of workgroups over the CUs times their length.
+// us with 1, 2, 4, 5 quads (BF16 logits, 64 biases, a mask; histories of 300 and 32768 tokens): 8 rows of 128256 4.5, 5.1, 6.2, 6.8
+// and 6.9, 7.9, 9.7, 10.9; 32 of 50257 6.3, 6.0, 7.2, 7.8 and 9.8, 8.9, 11.1, 12.1; 32 of 152064 12.9, 11.0, 10.0, 9.7 and 19.3, 15.8, 15.5,
+// 13.7 (24 MB read and written, 4 more of history: 2.3 TB/s; without a history 8.1: 3.7).  256 threads of four quads: 1 row of
+// 128256 5.0 and 10.8 against 3.9 and 5.9.
+// Tried and slower: a row's blocks of 64 logits dealt out among its workgroups, which spreads the frequent low token numbers but
+// takes twice the instructions per token; one LDS operation for up to four tokens of a lane; more tokens in flight.
 // Rows are the grid's fast axis: with a multiple of eight of them all ranges of a row run on one XCD, whose L2 then serves the
 // history.
-template <int kType, int kThreads, bool kWhole>
-__global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) {
-  constexpr int kRange = kThreads * 4 * kConQuads;
+template <int kType, int kQuads, bool kWhole>
+__global__ __launch_bounds__(kConThreads) void constrain_kernel(ConstrainLaunch a) {
+  constexpr int kThreads = kConThreads, kRange = kThreads * 4 * kQuads;
   constexpr int kValue = kType == kTypeFp32 ? 4 : 2;
   __shared__ con_u4 s_slot[kRange / 4];
   unsigned *slot = (unsigned *)s_slot;
@@ -81,13 +84,13 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   // first logit of the thread's quad k (-3 .. -1: a quad that begins ahead of the row; V and more: none)
   auto place = [&](int k) { return lo + 4 * (tid + k * kThreads); };
   // ---- requests ----
-  float x[kConQuads][4];
+  float x[kQuads][4];
   if (quads) {
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) load_quad<kType>(row, min(max(place(k), first_quad), last_quad), x[k]);
+    for (int k = 0; k < kQuads; ++k) load_quad<kType>(row, min(max(place(k), first_quad), last_quad), x[k]);
   } else {
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k)
+    for (int k = 0; k < kQuads; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[k][e] = logit_at<kType>(row, min(max(place(k) + e, 0), V - 1));
   }
@@ -104,16 +107,16 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
     if (a.presence) pres = a.presence[b];
     if (a.frequency) freq = a.frequency[b];
   }
-  typename std::conditional<kWhole, unsigned, unsigned long long>::type bits[kConQuads];   // the quad's mask bits, and what lies behind them
+  typename std::conditional<kWhole, unsigned, unsigned long long>::type bits[kQuads];   // the quad's mask bits, and what lies behind them
 #pragma unroll
-  for (int k = 0; k < kConQuads; ++k) bits[k] = 15u;
+  for (int k = 0; k < kQuads; ++k) bits[k] = 15u;
   if (a.allowed) {
     const int m = a.allowed_rows ? a.allowed_rows[b] : b;
     if (m >= 0 && m < a.n_masks) {
       const int words = (V + 31) / 32;
       const uint32_t *mask = a.allowed + (long long)m * words;
 #pragma unroll
-      for (int k = 0; k < kConQuads; ++k) {
+      for (int k = 0; k < kQuads; ++k) {
         // (a quad that starts ahead of the row takes its bits from the row's first word, moved up)
         const int i = place(k), w = min(max(i, 0) >> 5, words - 1);
         if constexpr (kWhole) {
@@ -134,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   // the row's first and last quad where they are no whole ones (behind the requests: what is loaded twice is waited for)
   if (!kWhole && quads) {
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) {
+    for (int k = 0; k < kQuads; ++k) {
       const int i = place(k);
       if (i < 0 || (i + 4 > V && i < V)) {
 #pragma unroll
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   // ---- the history's counts ----
   if (n > 0) {
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
+    for (int k = 0; k < kQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
     __syncthreads();
     // kind: 0 prompt, 1 generated, 2 either
     auto count = [&](int id, int i, auto kind) {
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) {
+    for (int k = 0; k < kQuads; ++k) {
       const con_u4 s = s_slot[tid + k * kThreads];
       if ((s.x | s.y | s.z | s.w) == 0u) continue;
 #pragma unroll
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
   if (b0 < b1) {
     // (a thread clears the slots that only it has read since the last barrier)
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
+    for (int k = 0; k < kQuads; ++k) s_slot[tid + k * kThreads] = con_u4{0u, 0u, 0u, 0u};
     __syncthreads();
     for (int i = b0 + tid; i < b1; i += kThreads) {
       const unsigned at = (unsigned)(i == b0 + tid ? bias_ahead : a.bias_tokens[i]) - (unsigned)lo;
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kConQuads; ++k) {
+    for (int k = 0; k < kQuads; ++k) {
       const con_u4 s = s_slot[tid + k * kThreads];
       if ((s.x | s.y | s.z | s.w) == 0u) continue;
 #pragma unroll
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
     }
   }
 #pragma unroll
-  for (int k = 0; k < kConQuads; ++k) {
+  for (int k = 0; k < kQuads; ++k) {
     const int i = place(k);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[k][e] = (bits[k] >> e) & 1u ? x[k][e] : -INFINITY;
@@ -248,14 +251,27 @@ __global__ __launch_bounds__(kThreads) void constrain_kernel(ConstrainLaunch a) 
 hipError_t launch_constrain(const ConstrainLaunch &a, int type, hipStream_t stream) {
   const size_t value = type == kTypeFp32 ? 4 : 2;
   const bool whole = a.V % 4 == 0 && a.row_stride % 4 == 0 && (uintptr_t)a.logits % (4 * value) == 0 && (uintptr_t)a.out % 16 == 0;
-  const int threads = a.tokens && a.max_tokens >= 2048 ? 512 : 256;      // (see the kernel)
-  const int range = threads * 4 * kConQuads;
+  // quads per thread: see the kernel
+  const long long cus = std::max(1, device_cu_count());
+  int quads = 1;
+  long long least = 0;
+  for (int q : {1, 2, 4, 5}) {
+    const int range = kConThreads * 4 * q;
+    const long long groups = (long long)a.B * ((a.V + 3 + range - 1) / range), cost = (groups + cus - 1) / cus * (q + 1);
+    if (q > 1 && cost >= least) continue;
+    least = cost;
+    quads = q;
+  }
+  const int range = kConThreads * 4 * quads;
   const dim3 grid(a.B, (a.V + 3 + range - 1) / range);     // (a row may start three places into its first quad)
-#define CONFKV_CASE(t, n) \
-  if (type == t && threads == n && whole) hipLaunchKernelGGL((constrain_kernel<t, n, true>), grid, dim3(n), 0, stream, a); \
-  if (type == t && threads == n && !whole) hipLaunchKernelGGL((constrain_kernel<t, n, false>), grid, dim3(n), 0, stream, a);
-  CONFKV_CASE(kTypeFp32, 256) CONFKV_CASE(kTypeFp16, 256) CONFKV_CASE(kTypeBf16, 256)
-  CONFKV_CASE(kTypeFp32, 512) CONFKV_CASE(kTypeFp16, 512) CONFKV_CASE(kTypeBf16, 512)
+#define CONFKV_CASE(q) \
+  if (quads == q) { \
+    auto fn = type == kTypeFp32 ? (whole ? constrain_kernel<kTypeFp32, q, true> : constrain_kernel<kTypeFp32, q, false>) \
+            : type == kTypeFp16 ? (whole ? constrain_kernel<kTypeFp16, q, true> : constrain_kernel<kTypeFp16, q, false>) \
+                                : (whole ? constrain_kernel<kTypeBf16, q, true> : constrain_kernel<kTypeBf16, q, false>); \
+    hipLaunchKernelGGL(fn, grid, dim3(kConThreads), 0, stream, a); \
+  }
+  CONFKV_CASE(1) CONFKV_CASE(2) CONFKV_CASE(4) CONFKV_CASE(5)
 #undef CONFKV_CASE
   return hipGetLastError();
 }

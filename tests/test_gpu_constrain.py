@@ -106,6 +106,7 @@ def _device(torch, c):
 @pytest.mark.parametrize("B,V,n,m,masks", [
     (1, 2, 1, 0, None), (1, 33, 0, 0, 1), (2, 31, 5, 3, 2), (3, 4096, 100, 40, 3), (2, 4097, 1000, 0, None),
     (1, 50257, 300, 17, 1), (5, 12007, 2, 1, 5), (2, 128256, 9000, 300, 2), (33, 1001, 64, 64, 33), (1, 152064, 40000, 1000, 1),
+    (32, 50257, 3000, 64, 32), (64, 50256, 500, 10, None), (85, 50257, 100, 90, 85), (85, 50256, 30, 0, None),   # two, four, five quads per thread
 ])
 def test_rows_match_the_formulas(lib, torch_cuda, dtype, B, V, n, m, masks):
     torch = torch_cuda
