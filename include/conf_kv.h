@@ -10,14 +10,18 @@
  *     once:             conf_kv_step            (confidence -> tight/loose budget)
  *     once:             conf_kv_evict_compact   (rank, evict, compact, demote)
  *
- * which is the paper's Algorithm 1 with the append moved in front of the step's own
+ * and, where a program wants them, conf_kv_prepare_qkv in front of the attention (projection rows ->
+ * queries, keys, values), conf_kv_attend_shared in its place (a prefix that sequences share) and
+ * conf_kv_constrain in front of conf_kv_step (penalties, biases, grammar masks).
+ *
+ * The first three are the paper's Algorithm 1 with the append moved in front of the step's own
  * attention (a decode query attends to its own key).
  *
  * Conventions
  *   - "dev" pointers are device memory owned by the CALLER and valid until
  *     conf_kv_destroy; "host" pointers are ordinary host memory.  The library never
  *     allocates or frees device memory.
- *   - The three hot calls only enqueue kernels on the given stream; they never
+ *   - The hot calls (those above) only enqueue kernels on the given stream; they never
  *     synchronise.  Lengths and budgets live on the device; the host keeps upper bounds.
  *   - A handle is driven from one host thread, on one stream at a time.
  *   - A whole decode step (the calls above, on one stream) may be recorded into a HIP graph

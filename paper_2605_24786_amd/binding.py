@@ -382,7 +382,7 @@ class ConfKV:
             m = bias_tokens.numel()
         if allowed is not None:
             masks = allowed.shape[0]
-            if allowed.dtype is not i32:
+            if allowed.dtype is self._torch.uint32:
                 allowed = allowed.view(i32)
         args = _CONSTRAINTS.pack(
             kind, n, logits.data_ptr(), apart if B > 1 else V, want("out", out, f32, (B, V)), ids, ids_apart,

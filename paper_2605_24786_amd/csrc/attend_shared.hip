@@ -72,7 +72,7 @@ template <int D>
 struct SharedRowsState {
   sh_h8 qf[D / 16];
   sh_f16 O[D / 32];
-  float mref, l;                                       // reference in units of the raw score; per-lane partial sum
+  float mref, l;                                       // reference in units of the raw score; per-lane partial sum (lifted, as O)
   int lim, least, most;                                // keys the lane's row sees; the fewest and the most of the 32 rows
 
   __device__ __forceinline__ void reset() {
@@ -89,7 +89,7 @@ struct SharedRowsState {
   __device__ __forceinline__ void take(const uint8_t *Kt, const uint8_t *Vt, int key0, bool bad, const __half *V, int T, float sm) {
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5, t16 = lane & 15, c2 = (lane >> 4) & 1;
     const float NEG = -INFINITY, c = sm * 1.44269504088896341f;
-    constexpr float kSlack = 4.0f;
+    constexpr float kSlack = 4.0f, kLift = 10.0f;
     sh_f16 sc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[i] = 0.f;
@@ -107,7 +107,7 @@ struct SharedRowsState {
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
     // The reference only has to stay near the maximum (the merge is exact for any), so the exchange and the rescaling run
-    // where a score passes it by more than kSlack; e^kSlack times the largest fp16 value is far inside float32.
+    // where a score passes it by more than kSlack.
     if (__builtin_amdgcn_ballot_w64((mx - mref) * sm > kSlack)) {
       const float mn = fmaxf(mref, fmaxf(mx, other_half(mx)));
       const float corr = mn == NEG ? 1.f : __builtin_amdgcn_exp2f((mref - mn) * c);
@@ -116,8 +116,10 @@ struct SharedRowsState {
 #pragma unroll
       for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
     }
-    // (the rounding of mref * c is the same for all keys of the row: it only scales m, by less than the scores' own rounding)
-    const float ref = mref == NEG ? 0.f : mref * c;
+    // Probabilities are held 2^10 times as large, at most 55910 of fp16's 65504: as fp16 operands they keep eleven bits down to
+    // 6e-8 (unscaled 6e-5, which the tail of a long prefix is below).  (The rounding of mref * c is the same for all keys of
+    // the row: it only scales m, by less than the scores' own rounding.)
+    const float ref = (mref == NEG ? 0.f : mref * c) - kLift;
     sh_h8 pb[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -162,6 +164,7 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
   constexpr int PR = D / 8;                              // 16-byte pieces of a row
   constexpr int TK = L::TK;
   constexpr int kLoaders = RW == 1 ? kWave : kShThreads; // lanes that share the loads of kRowsLoaded keys
+  constexpr float kUnlift = 0x1p-10f;                    // see SharedRowsState::take
   constexpr int kRowsLoaded = RW == 1 ? kShKeys : TK, NP = kRowsLoaded * PR / kLoaders, kStep = kLoaders / PR;
   __shared__ __align__(16) uint8_t s_tile[L::kBytes];
   __shared__ float s_m[kShWaves][kShRows], s_l[kShWaves][kShRows];
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
       if (base + TK < hi) take_turn(x, turn + 1, base + TK);
     }
   }
-  st.l += other_half(st.l);
+  st.l = (st.l + other_half(st.l)) * kUnlift;
   // (-inf stays; where every score was NaN the maximum saw none: +inf lets the merges give NaN)
   if (h == 0) {
     s_m[w][l32] = st.mref == NEG && st.l != st.l ? INFINITY : st.mref * a.sm_scale;
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *(float4 *)(wo + l32 * L::OROW + 32 * nt + 8 * i + 4 * h) =
-          make_float4(st.O[nt][4 * i], st.O[nt][4 * i + 1], st.O[nt][4 * i + 2], st.O[nt][4 * i + 3]);
+          make_float4(st.O[nt][4 * i] * kUnlift, st.O[nt][4 * i + 1] * kUnlift, st.O[nt][4 * i + 2] * kUnlift, st.O[nt][4 * i + 3] * kUnlift);
   __syncthreads();
   // sixteen threads per row merge the partials of the wavefronts along the keys
   const int row = tid >> 4;

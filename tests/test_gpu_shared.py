@@ -209,6 +209,30 @@ def test_sharp_scores(lib, torch_cuda, monkeypatch):
         c.close()
 
 
+@pytest.mark.parametrize("row_waves", [1, 4])
+@pytest.mark.parametrize("lead", [11.0, 14.0])
+def test_long_tails_of_small_probabilities(lib, torch_cuda, monkeypatch, row_waves, lead):
+    """One key leads all others by `lead`: 20000 equal probabilities of e^-lead (1.7e-5 and 8e-7) hold a quarter or a sixtieth of
+    the weight, and their rounding as operands has the same sign for all of them."""
+    torch, T, D = torch_cuda, 20000, 128
+    c = _Case(lib, torch, monkeypatch, D, 4, 1, 2, T, 20, 16, seed=2, row_waves=row_waves)
+    c.pk[:], c.pv[:] = 0, 1
+    c.pk[0, 77, 0], c.pv[0, 77] = 4.0, -1
+    c.shared[0].copy_(c.on(c.pk))
+    c.shared[1].copy_(c.on(c.pv))
+    q, kn, vn = c.inputs()
+    q[:], kn[:] = 0, 0
+    q[..., 0] = lead * math.sqrt(D) / 4.0
+    out = torch.empty(2, 1, 4, D, dtype=torch.float16, device="cuda")
+    c.kv.attend_shared(0, c.on(q), c.on(kn), c.on(vn), out, *c.shared)
+    got = out.cpu().numpy().astype(np.float64)
+    for (b, g), u in c.units.items():
+        ref, tol = _attend(u, q[b], kn[b, :, 0], vn[b, :, 0], 20, c.pk[0], c.pv[0], f32(1 / math.sqrt(D)), f32(0.9))
+        err = np.abs(got[b] - ref) / tol
+        assert np.all(err <= 1.0), f"{err.max():.3g} x tolerance"
+    c.close()
+
+
 @pytest.mark.parametrize("row_waves", [1, 2, 4])
 @pytest.mark.parametrize("kind", ["inf value", "nan value", "nan key", "inf key"])
 def test_odd_values_reach_only_those_who_see_them(lib, torch_cuda, monkeypatch, kind, row_waves):
