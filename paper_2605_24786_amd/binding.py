@@ -324,10 +324,10 @@ class ConfKV:
         if t is None:
             return 0, 0, 0
         B, D = self._batch, self._head_dim
-        sb, st, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
         if t.dtype is not dtype or t.shape != (B, tokens, heads, D) or t.get_device() != self._device:
             raise ValueError(f"{name}: {dtype} [{B}][{tokens}][{heads}][{D}] on {self.state.device} is wanted, got {t.dtype} "
                              f"{tuple(t.shape)} on {t.device}")
+        sb, st, sh, sd = t.stride()
         if (sd != 1 or (sh != D and heads > 1)) and tokens:
             raise ValueError(f"{name}: the heads of a token are dense, got strides {t.stride()}")
         return t.data_ptr(), sb if B > 1 else 0, st if tokens > 1 else 0      # (a size of 1 may come with any stride)
@@ -340,17 +340,19 @@ class ConfKV:
         pos * freq, one rounding.  pos int32 [B][T], or None: the positions the next appended tokens of the layer get; `first` is
         added.  Each of q, k and v may be None together with its destination."""
         like = q if q is not None else k if k is not None else v
-        if like is None or like.dim() != 4 or like.dtype not in self._type:
+        shape, dtype = (like.shape, like.dtype) if like is not None else ((), None)
+        kind = self._type.get(dtype)
+        if len(shape) != 4 or kind is None:
             raise ValueError("prepare_qkv: q, k or v [B][T][heads][D] of float32, float16 or bfloat16 is wanted")
-        B, H, Hq, D, want = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._want
-        half, f32, dtype = self._half, self._f32, like.dtype
-        T = like.shape[1]
-        qp, qb, qt = self._rows("q", q, dtype, T, Hq)
-        kp, kb, kt = self._rows("k", k, dtype, T, H)
-        vp, vb, vt = self._rows("v", v, dtype, T, H)
+        B, H, Hq, D, want, rows_of = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._want, self._rows
+        half, f32 = self._half, self._f32
+        T = shape[1]
+        qp, qb, qt = rows_of("q", q, dtype, T, Hq)
+        kp, kb, kt = rows_of("k", k, dtype, T, H)
+        vp, vb, vt = rows_of("v", v, dtype, T, H)
         rows = (B, H, T, D) if prompt else (B, T, H, D)
         pairs = 0 if freq is None else freq.numel()
-        args = _QKV.pack(T, self._type[dtype], qp, kp, vp, qb, qt, kb, kt, vb, vt, want("q_weight", q_weight, f32, (D,)),
+        args = _QKV.pack(T, kind, qp, kp, vp, qb, qt, kb, kt, vb, vt, want("q_weight", q_weight, f32, (D,)),
                          want("k_weight", k_weight, f32, (D,)), want("freq", freq, f32, (pairs,)),
                          want("pos", pos, self._i32, (B, T)), first, 2 * pairs, 1 if interleaved else 0, 1 if prompt else 0, eps,
                          want("q16", q16, half, (B, T, Hq, D)), want("k16", k16, half, rows), want("v16", v16, half, rows))
