@@ -438,7 +438,7 @@ typedef struct conf_kv_constraints {
   const int32_t *dev_bias_tokens;   /* int32 [n_bias]                                                          */
   const float *dev_bias_values;     /* fp32 [n_bias]: added (-inf bans a token); of several entries of one row
                                        for one token the last one counts                                       */
-  int32_t n_bias;                   /* entries there are; offsets are held within 0 .. n_bias                  */
+  int32_t n_bias;                   /* entries there are, up to 2^30; offsets are held within 0 .. n_bias       */
   int32_t n_masks;                  /* rows of dev_allowed                                                     */
   const uint32_t *dev_allowed;      /* uint32 [n_masks][ceil(V / 32)]: bit v & 31 of word v / 32 set = allowed  */
   const int32_t *dev_allowed_rows;  /* int32 [B]: the mask row of each sequence, one outside 0 .. n_masks - 1
@@ -451,9 +451,10 @@ typedef struct conf_kv_constraints {
  *     x <- x > 0 ? x / repetition : x * repetition       where the token is in the history
  *     x <- x - frequency * count - presence               where it was generated, count times
  *     x <- x + bias;   x <- -inf where it is forbidden
- * in float32.  (Nothing happens to the history's tokens with max_tokens 0.)  A row that forbids everything is all -inf; conf_kv_step then gives a confidence that is NaN and the loose
- * budget.  Penalties need dev_tokens and dev_lengths; lengths, offsets, ids and mask rows are held within
- * the arrays' bounds on the device.  At most 2^27 logits a row (CONF_KV_ERR_BAD_SHAPE).  The result does not depend on the order in which workgroups run. */
+ * in float32.  A row that forbids everything is all -inf; conf_kv_step then gives a confidence that is NaN and the loose
+ * budget.  Penalties need dev_tokens and dev_lengths (with max_tokens 0 neither, and they do nothing); lengths, offsets, ids and
+ * mask rows are held within the arrays' bounds on the device.  At most 2^27 logits a row (CONF_KV_ERR_BAD_SHAPE).  The result
+ * does not depend on the order in which workgroups run. */
 int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_kv_stream stream);
 
 /*

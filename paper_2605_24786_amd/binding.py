@@ -382,7 +382,12 @@ class ConfKV:
             raise ValueError("tokens: penalties need the history")
         if bias_tokens is not None:
             m = bias_tokens.numel()
-        if allowed is not None:
+        if (bias_offsets is None) != (bias_tokens is None) or (bias_tokens is None and bias_values is not None):
+            raise ValueError("biases: offsets, tokens and values are wanted together")
+        if allowed is None:
+            if allowed_rows is not None:
+                raise ValueError("allowed_rows: there is no `allowed` that it chooses from")
+        else:
             masks = allowed.shape[0]
             if allowed.dtype is self._torch.uint32:
                 allowed = allowed.view(i32)

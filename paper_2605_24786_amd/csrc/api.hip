@@ -669,7 +669,7 @@ int conf_kv_constrain(conf_kv_handle *h, const conf_kv_constraints *args, conf_k
   if (V > 1 << 27) return CONF_KV_ERR_BAD_SHAPE;
   if (penalties && (c.max_tokens < 0 || c.max_tokens > 1 << 30 || (c.max_tokens > 0 && (!c.dev_tokens || !c.dev_lengths || c.tokens_stride < c.max_tokens))))
     return CONF_KV_ERR_INVALID_ARG;
-  if (c.dev_bias_offsets && (c.n_bias < 0 || (c.n_bias > 0 && (!c.dev_bias_tokens || !c.dev_bias_values)))) return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_bias_offsets && (c.n_bias < 0 || c.n_bias > 1 << 30 || (c.n_bias > 0 && (!c.dev_bias_tokens || !c.dev_bias_values)))) return CONF_KV_ERR_INVALID_ARG;
   if (c.dev_allowed && (c.n_masks < 0 || (!c.dev_allowed_rows && c.n_masks < B))) return CONF_KV_ERR_INVALID_ARG;
   if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
   ConstrainLaunch a{};

@@ -227,3 +227,22 @@ def test_refusals(lib, torch_cuda):
         with pytest.raises(ValueError):
             kv.constrain(*args, **kw)
     kv.close()
+
+
+def test_parts_that_would_do_nothing_are_refused(lib, torch_cuda):
+    """Half a list of biases, a choice among no masks, more biases than indexes are made for."""
+    torch = torch_cuda
+    B, V = 2, 100
+    kv = _kv(lib, B, V)
+    x, out = torch.zeros(B, V, device="cuda"), torch.zeros(B, V, device="cuda")
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    offsets, ids, values = i32(0, 1, 2), i32(1, 2), torch.ones(2, device="cuda")
+    for kw in (dict(bias_tokens=ids, bias_values=values), dict(bias_offsets=offsets), dict(bias_values=values),
+               dict(bias_offsets=offsets, bias_values=values), dict(allowed_rows=i32(0, 1))):
+        with pytest.raises(ValueError):
+            kv.constrain(x, out, **kw)
+    from paper_2605_24786_amd import binding as b
+    args = b._CONSTRAINTS.pack(b.TYPE_FP32, 0, x.data_ptr(), V, out.data_ptr(), 0, 0, 0, 0, 0, 0, 0, offsets.data_ptr(), ids.data_ptr(),
+                               values.data_ptr(), 2 ** 30 + 1, 0, 0, 0)
+    assert kv.lib.conf_kv_constrain(kv.h, args, kv._stream()) == b.ERR_INVALID_ARG
+    kv.close()
