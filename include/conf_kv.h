@@ -415,8 +415,8 @@ typedef struct conf_kv_qkv {
  * and is rounded to fp16 once; values are rounded to fp16.  Angles are formed in float64, norms and products in float32.  What
  * is beyond fp16's range becomes infinite.  Each of q, k and v may be left out (source and destination NULL), not all.
  * The handle gives B, Hq, Hkv, D and, with dev_pos NULL, the positions, which live on the device: a recorded call moves on
- * with the cache.  Nothing of the cache changes.  Tensors are 16-byte aligned and so are the strides in bytes; destinations
- * overlap no source.  B * T at most 2^30. */
+ * with the cache.  Nothing of the cache changes.  Tensors are 16-byte aligned and so are the strides in bytes; destinations lie
+ * apart from each other and from the sources (what is between a source's first and last value).  B * T at most 2^30. */
 int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *args, conf_kv_stream stream);
 
 /* Arguments of conf_kv_constrain.  NULL leaves a part out. */

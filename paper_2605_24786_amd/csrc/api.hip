@@ -611,12 +611,15 @@ int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *arg
       return CONF_KV_ERR_INVALID_ARG;
   }
   if (!given) return CONF_KV_ERR_INVALID_ARG;
+  auto written = [&](const Part &p) { return (size_t)B * T * p.heads * D * 2; };
   for (const Part &d : parts) {
     if (!d.dst) continue;
-    const size_t written = (size_t)B * T * d.heads * D * 2;
-    for (const Part &p : parts)
-      if (p.src && overlap(p.src, ((B - 1) * (size_t)p.batch + (T - 1) * (size_t)p.token + (size_t)p.heads * D) * vb, d.dst, written))
+    for (const Part &p : parts) {
+      if (!p.src) continue;
+      if (overlap(p.src, ((B - 1) * (size_t)p.batch + (T - 1) * (size_t)p.token + (size_t)p.heads * D) * vb, d.dst, written(d)))
         return CONF_KV_ERR_INVALID_ARG;
+      if (&p != &d && overlap(p.dst, written(p), d.dst, written(d))) return CONF_KV_ERR_INVALID_ARG;
+    }
   }
   if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
   PrepareLaunch a{};

@@ -200,3 +200,22 @@ def test_refusals(lib, torch_cuda):
     with pytest.raises(ValueError):
         kv.prepare_qkv(0, None, None, None)
     kv.close()
+
+
+def test_destinations_that_overlap_are_refused(lib, torch_cuda):
+    torch = torch_cuda
+    B, T, H, D = 2, 3, 2, 64
+    kv = _kv(lib, B, H, H, D)
+    q, k, v = torch.randn(3, B, T, H, D, device="cuda").half()
+    n = q.numel()
+    room = torch.empty(3 * n, dtype=torch.float16, device="cuda")
+    at = lambda i: room[i:i + n].view(B, T, H, D)
+    from paper_2605_24786_amd import binding as b
+    for places in ((0, 0, n), (0, n, n), (0, n, 2 * n - 8), (8, 0, 2 * n)):
+        with pytest.raises(lib.ConfKVError) as e:
+            kv.prepare_qkv(0, q, k, v, *(at(i) for i in places))
+        assert e.value.status == b.ERR_INVALID_ARG
+    kv.prepare_qkv(0, q, k, v, at(2 * n), at(0), at(n))                         # side by side
+    for i, x in ((2 * n, q), (0, k), (n, v)):
+        assert torch.equal(at(i), x)
+    kv.close()
