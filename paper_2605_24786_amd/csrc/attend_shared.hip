@@ -158,6 +158,8 @@ struct SharedRowsState {
 // tile or two, the merge).  With up to 32 rows (RW = 1) a wavefront waits for nobody before the merge: it loads and multiplies
 // tiles of its own, the next one in flight in registers while this one is used.  More rows share a turn's tiles through LDS, two
 // buffers, one barrier per turn, the two turns after the next in flight.
+// Its loads are streaming ones although several workgroups may read a line: plain loads took 17.9 us instead of 12.7 (8192 tokens, 32
+// rows), 21.1 instead of 13.4 (4096, 128) and 61.5 instead of 40.1 (32001, 80).
 template <int D, int RW>
 __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_prefix_kernel(SharedLaunch a, int blocks, int each) {
   using L = SharedTile<D, RW>;
