@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "confkv_dev.h"
+#include "constrain_ranges.h"
 #include "launch.h"
 
 namespace confkv {
@@ -76,11 +77,12 @@ __global__ __launch_bounds__(kConThreads) void constrain_kernel(ConstrainLaunch 
   unsigned *slot = (unsigned *)s_slot;
   const int b = blockIdx.x, tid = threadIdx.x, V = a.V;
   float *out = a.out + (long long)b * V;
-  const int off = kWhole ? 0 : (int)(((uintptr_t)out >> 2) & 3);
+  const int off = kWhole ? 0 : con_off((uintptr_t)out);
+  const int lo = con_first(blockIdx.y, off, kRange);
+  if (con_empty(lo, V)) return;
   const char *row = (const char *)a.logits + (long long)b * a.row_stride * kValue;
   const bool quads = kWhole || (((uintptr_t)(row - off * kValue) & (4 * kValue - 1)) == 0 && V >= 8);
   const int first_quad = (4 - off) & 3, last_quad = ((V - 4 + off) & ~3) - off;   // whole quads of the row: the first and the last
-  const int lo = (int)blockIdx.y * kRange - off;
   // first logit of the thread's quad k (-3 .. -1: a quad that begins ahead of the row; V and more: none)
   auto place = [&](int k) { return lo + 4 * (tid + k * kThreads); };
   // ---- requests ----
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(kConThreads) void constrain_kernel(ConstrainLaunch 
     }
   }
   // Token id's slot is id - lo.  (An id of -3 .. -1 may find a slot ahead of the row: nothing reads it.)
-  const unsigned size = (unsigned)min(kRange, V - lo);
+  const unsigned size = (unsigned)con_size(lo, V, kRange);
   n = min(max(n, 0), a.max_tokens);
   // ---- the history's counts ----
   if (n > 0) {
@@ -256,14 +258,13 @@ hipError_t launch_constrain(const ConstrainLaunch &a, int type, hipStream_t stre
   int quads = 1;
   long long least = 0;
   for (int q : {1, 2, 4, 5}) {
-    const int range = kConThreads * 4 * q;
-    const long long groups = (long long)a.B * ((a.V + 3 + range - 1) / range), cost = (groups + cus - 1) / cus * (q + 1);
+    const long long groups = (long long)a.B * con_grid_ranges((uintptr_t)a.out, a.B, a.V, kConThreads * 4 * q, whole);
+    const long long cost = (groups + cus - 1) / cus * (q + 1);
     if (q > 1 && cost >= least) continue;
     least = cost;
     quads = q;
   }
-  const int range = kConThreads * 4 * quads;
-  const dim3 grid(a.B, (a.V + 3 + range - 1) / range);     // (a row may start three places into its first quad)
+  const dim3 grid(a.B, con_grid_ranges((uintptr_t)a.out, a.B, a.V, kConThreads * 4 * quads, whole));
 #define CONFKV_CASE(q) \
   if (quads == q) { \
     auto fn = type == kTypeFp32 ? (whole ? constrain_kernel<kTypeFp32, q, true> : constrain_kernel<kTypeFp32, q, false>) \

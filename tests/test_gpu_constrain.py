@@ -246,3 +246,31 @@ def test_parts_that_would_do_nothing_are_refused(lib, torch_cuda):
                                values.data_ptr(), 2 ** 30 + 1, 0, 0, 0)
     assert kv.lib.conf_kv_constrain(kv.h, args, kv._stream()) == b.ERR_INVALID_ARG
     kv.close()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("B,V", [(1, 4094), (1, 4095), (3, 4094), (5, 4095), (2, 8190), (1, 8191), (3, 8191), (1, 32767), (2, 32768),
+                                 (40, 32766), (1, 131072), (33, 122879), (256, 20479)])
+def test_vocabularies_that_end_at_a_range(lib, torch_cuda, dtype, B, V):
+    """Rows that end where a workgroup's range does or one to three logits ahead of it, the result on a 16-byte boundary and one,
+    two and three places behind it; histories and biases that name the first and the last tokens."""
+    torch = torch_cuda
+    print(f"constrain {dtype} B={B} V={V}", flush=True)
+    c = _case(B, V, 60, 3 * B, seed=V + B, masks=2 if B == 2 else None)
+    c["tokens"][:, 10:14], c["tokens"][:, 14:18] = np.arange(4), V - 1 - np.arange(4)
+    c["lengths"][:] = 60
+    c["prompt_lengths"] = np.full(B, 12, np.int32)
+    c["bias_offsets"] = 3 * np.arange(B + 1, dtype=np.int32)
+    c["bias_tokens"][0::3], c["bias_tokens"][1::3] = 0, V - 1
+    x = torch.from_numpy(c["logits"]).to(getattr(torch, dtype)).cuda()
+    ref, size = _expected(c, x.float().cpu().numpy())
+    kv = _kv(lib, B, V)
+    kw = _device(torch, c)
+    for places in range(4):
+        room = torch.full((B * V + 8,), 9.0, device="cuda")
+        out = room[places:places + B * V].view(B, V)
+        kv.constrain(x, out, **kw)
+        torch.cuda.synchronize()
+        _check(out.cpu().numpy(), ref, size, f"{places} places behind a boundary")
+        assert bool((room[:places] == 9).all()) and bool((room[places + B * V:] == 9).all())
+    kv.close()
