@@ -903,7 +903,8 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
       for (int q = 0; q < kOut; ++q) {
         const int os = sub + (q << lgl);
         const float wgt = mine && os < ns ? pml[(h << lg) + os] : 0.f;   // e^{m_s - M} / L of that split and row
-        c += wgt > 0.f ? __uint_as_float((unsigned)opre[q]) * wgt : 0.f;   // (an empty partial may hold anything)
+        // (an empty partial may hold anything; a weight that is NaN, from a score that is none, must show)
+        c += wgt != 0.f ? __uint_as_float((unsigned)opre[q]) * wgt : 0.f;
       }
       c = group_sum(c, 1 << lgl);
       if (mine && sub == 0 && h < tq * gq && a.out && e - h * D < DR)

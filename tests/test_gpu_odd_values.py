@@ -1,0 +1,59 @@
+"""Keys and values that are no numbers in decode attention, with and without a shared prefix: what a sequence sees of them shows in its
+output, whatever the number of splits and wavefronts, and whatever the other sequences see.
+
+  a key that is NaN       its score and with it every probability of the row is NaN: the whole output is
+  a value v, |v| = inf    p v = v for every probability p > 0, however small: the output's channel is v, NaN where both infinities meet
+  a value that is NaN     the output's channel is NaN"""
+import math
+import os
+import sys
+
+import numpy as np
+import pytest
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+from test_gpu_shared import _Case  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch_cuda():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch
+
+
+_FORMS = [(128, 4, 1), (128, 1, 1), (64, 4, 1), (64, 1, 1), (128, 16, 1), (128, 4, 3)]
+
+
+def _out(c, prefix, q, kn, vn):
+    torch = c.torch
+    out = torch.zeros(c.B, c.tq, c.H * c.G, c.D, dtype=torch.float16, device="cuda")
+    x = [c.on(z) for z in (q, kn, vn)]
+    if prefix:
+        seen = None if c.seen is None else c.on(np.array(c.seen, np.int32))
+        c.kv.attend_shared(0, *x, out, *c.shared, seen=seen)
+    elif c.tq > 1:
+        c.kv.attend_chunk(0, *x, out)
+    else:
+        c.kv.attend(0, *x, out)
+    got = out.cpu().numpy().astype(np.float64)
+    assert c.kv.counters().device_errors == 0
+    return got
+
+
+@pytest.mark.parametrize("splits,two_launch", [(1, False), (3, False), (4, True)])
+@pytest.mark.parametrize("prefix,D,G,tq", [(False, 128, 8, 4)] + [(p, *f) for p in (False, True) for f in _FORMS])
+def test_own_key_not_a_number(lib, torch_cuda, monkeypatch, prefix, D, G, tq, splits, two_launch):
+    """The call's last key is NaN, in a cache of 700 tokens on several splits: nothing but NaN for the token that sees it."""
+    c = _Case(lib, torch_cuda, monkeypatch, D, G, 2, 2, 300, 700, -1, tq=tq, splits=splits, two_launch=two_launch, seed=G)
+    q, kn, vn = c.inputs()
+    kn[0, -1, 1, 5] = math.nan
+    got = _out(c, prefix, q, kn, vn)
+    hit = np.zeros(got.shape, bool)
+    hit[0, -1, G:] = True
+    assert np.array_equal(np.isnan(got), hit) and np.isfinite(got[~hit]).all()
+    ema = c.kv.export(0, 0, 1)["ema"], c.kv.export(0, 0, 0)["ema"], c.kv.export(0, 1, 1)["ema"]
+    assert np.isnan(ema[0]).all() and np.isfinite(ema[1]).all() and np.isfinite(ema[2]).all()
+    c.close()
