@@ -565,6 +565,10 @@ __device__ __forceinline__ double recip_pos(double x) {
   return r * (2.0 - x * r);
 }
 
+// The maximum of a partial result for the merges.  Maxima pass a NaN by, so one that met nothing but scores that are no numbers has
+// that of a partial without slots, which weighs nothing; its sum is NaN, and +inf lets it outweigh the others.
+__device__ __forceinline__ float shown_maximum(float m, float l) { return l == l ? m : INFINITY; }
+
 // ---------------------------------------------------------------------------------------
 // A shared prefix (conf_kv_attend_shared): its partial results, formed by an earlier launch, join the wavefronts' own before
 // those are stored.  Part p of a unit goes to wavefront p of its ns * 8, and on; everything behind (merge, exchange, importance,
@@ -586,6 +590,8 @@ __device__ __forceinline__ void take_shared_valu(const AttendLaunch &a, const Sl
   constexpr int LPT = D / 16;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   if (lane >= LPT) return;
+#pragma unroll
+  for (int h = 0; h < G; ++h) st.m[h] = shown_maximum(st.m[h], st.l[h]);
   for (int p = sl.j * kAttWaves + w; p < a.shared_parts; p += ns * kAttWaves) {
     const size_t at = ((size_t)sl.ul * a.shared_parts + p) * G;
 #pragma unroll
@@ -704,7 +710,7 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
       const int at = min(64 * b + lane8, G * NP - 1);  // (lanes past the last row repeat its last partial; nothing reads them)
-      const float mk = wm[at], lk = wl[at];
+      const float lk = wl[at], mk = shown_maximum(wm[at], lk);
       row_m[b] = group_max(mk, 8);
       const bool live = mk > NEG;                      // an empty partial may hold anything and weighs nothing
       part_w[b] = live ? __expf(mk - row_m[b]) : 0.f;
@@ -1795,6 +1801,7 @@ void attend_mfma_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t
       unbias[j] = (kRows ? rows4_sum(pbias[j]) : row16_sum(pbias[j])) * kCodeBias;
       pbias[j] = 0.f;
       lrun[j] = kRows ? rows4_sum(lrun[j]) : row16_sum(lrun[j]);
+      mrun[j] = shown_maximum(mrun[j], lrun[j]);
     }
     const float bias = head_of_column<G>(unbias, t16);
 #pragma unroll

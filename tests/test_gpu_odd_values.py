@@ -57,3 +57,20 @@ def test_own_key_not_a_number(lib, torch_cuda, monkeypatch, prefix, D, G, tq, sp
     ema = c.kv.export(0, 0, 1)["ema"], c.kv.export(0, 0, 0)["ema"], c.kv.export(0, 1, 1)["ema"]
     assert np.isnan(ema[0]).all() and np.isfinite(ema[1]).all() and np.isfinite(ema[2]).all()
     c.close()
+
+
+@pytest.mark.parametrize("T0", [0, 1, 8, 16, 32, 64, 128, 256])
+@pytest.mark.parametrize("prefix,D,G,tq", [(False, 128, 8, 4)] + [(p, *f) for p in (False, True) for f in _FORMS])
+def test_own_key_not_a_number_in_a_tile_of_its_own(lib, torch_cuda, monkeypatch, prefix, D, G, tq, T0):
+    """The call's first key is NaN and, at some of these lengths, the only one that its wavefront meets, so that the wavefront's
+    largest score is that of one that met nothing; the other wavefronts, or the prefix, have numbers."""
+    for T in (1, 700) if prefix else (1,):
+        c = _Case(lib, torch_cuda, monkeypatch, D, G, 2, 2, T, T0, -1, tq=tq, seed=T0)
+        q, kn, vn = c.inputs()
+        kn[1, 0, 0, 7] = math.nan
+        got = _out(c, prefix, q, kn, vn)
+        hit = np.zeros(got.shape, bool)
+        hit[1, :, :G] = True
+        assert np.array_equal(np.isnan(got), hit) and np.isfinite(got[~hit]).all(), T
+        assert np.isnan(c.kv.export(0, 1, 0)["ema"]).all() and np.isfinite(c.kv.export(0, 1, 1)["ema"]).all(), T
+        c.close()
