@@ -309,9 +309,9 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
     }
   }
   st.l = (st.l + other_half(st.l)) * kUnlift;
-  // (-inf stays; where every score was NaN the maximum saw none: +inf lets the merges give NaN)
+  // (-inf stays; a sum that is NaN, from a score that is none, outweighs the others: a merge shall not lose it to larger scores)
   if (h == 0) {
-    s_m[w][l32] = st.mref == NEG && st.l != st.l ? INFINITY : st.mref * a.sm_scale;
+    s_m[w][l32] = st.l == st.l ? st.mref * a.sm_scale : INFINITY;
     s_l[w][l32] = st.l;
   }
   // The partials take the tiles' room: with RW = 1 a wavefront's own tile, which nobody else reads, else any.

@@ -74,3 +74,54 @@ def test_own_key_not_a_number_in_a_tile_of_its_own(lib, torch_cuda, monkeypatch,
         assert np.array_equal(np.isnan(got), hit) and np.isfinite(got[~hit]).all(), T
         assert np.isnan(c.kv.export(0, 1, 0)["ema"]).all() and np.isfinite(c.kv.export(0, 1, 1)["ema"]).all(), T
         c.close()
+
+
+_LAUNCHES = [(1, False), (3, False), (3, True)]
+
+
+def _leading(c, lead, where, at):
+    """Queries that score 0 with every key but one, which leads them by `lead`: the prefix's key `at`, or the call's own."""
+    q, kn, vn = c.inputs()
+    q[:], kn[:], c.pk[:] = 0, 0, 0
+    q[..., 0] = 16
+    key = np.float16(lead * math.sqrt(c.D) / 16)
+    if where == "prefix":
+        c.pk[:, at, 0] = key
+    else:
+        kn[..., 0] = key
+    return q, kn, vn
+
+
+def _share(c):
+    c.shared[0].copy_(c.on(c.pk))
+    c.shared[1].copy_(c.on(c.pv))
+
+
+@pytest.mark.parametrize("splits,two_launch", _LAUNCHES)
+@pytest.mark.parametrize("row_waves", [1, 2, 4])
+@pytest.mark.parametrize("D,G,tq", _FORMS)
+def test_prefix_key_not_a_number_behind_larger_scores(lib, torch_cuda, monkeypatch, D, G, tq, row_waves, splits, two_launch):
+    """Scores 150 above all others, in the prefix and in the cache, beside which the weight of the part with the NaN vanishes in
+    float32; a cache of 200 tokens, and one of which a wavefront has all."""
+    for where, T, T0 in (("prefix", 1500, 200), ("own", 1500, 200), ("prefix", 100, 0), ("own", 100, 0)):
+        c = _Case(lib, torch_cuda, monkeypatch, D, G, 1, 2, T, T0, -1, tq=tq, splits=splits, two_launch=two_launch, row_waves=row_waves)
+        q, kn, vn = _leading(c, 150.0, where, T - 1)
+        c.pk[0, 9, 1] = math.nan
+        _share(c)
+        c.seen = [T, 9]
+        got = _out(c, True, q, kn, vn)
+        assert np.isnan(got[0]).all() and np.isfinite(got[1]).all(), (where, T)
+        c.close()
+
+
+@pytest.mark.parametrize("splits,two_launch", _LAUNCHES)
+@pytest.mark.parametrize("D,G,tq", _FORMS)
+def test_own_key_not_a_number_behind_a_larger_prefix(lib, torch_cuda, monkeypatch, D, G, tq, splits, two_launch):
+    for T, T0 in ((1500, 200), (100, 1)):
+        c = _Case(lib, torch_cuda, monkeypatch, D, G, 1, 2, T, T0, -1, tq=tq, splits=splits, two_launch=two_launch)
+        q, kn, vn = _leading(c, 150.0, "prefix", T // 2)
+        kn[1, 0, 0, 2] = math.nan
+        _share(c)
+        got = _out(c, True, q, kn, vn)
+        assert np.isnan(got[1]).all() and np.isfinite(got[0]).all(), T
+        c.close()
