@@ -508,7 +508,7 @@ __device__ __forceinline__ void stream_fp16_valu(const CacheView &cv, const Atte
 
 // Merge the slot lane-groups of a wavefront and store the wavefront's partial
 // (m, l, o[G][D]) as entry `pidx` of the workgroup's LDS partial arrays.
-template <int D, int G>
+template <int D, int G, bool kShared = false>
 __device__ __forceinline__ void store_stream_partial(Stream<G> &st, int pidx, float *wm, float *wl,
                                                      float *wo_p) {
   constexpr int LPT = D / 16;
@@ -518,7 +518,8 @@ __device__ __forceinline__ void store_stream_partial(Stream<G> &st, int pidx, fl
 #pragma unroll
   for (int h = 0; h < G; ++h) {
     const float mw = wave_max(st.m[h]);
-    const float f = (st.m[h] == NEG) ? 0.f : __expf(st.m[h] - mw);
+    float f = (st.m[h] == NEG) ? 0.f : __expf(st.m[h] - mw);
+    if constexpr (kShared) f = (st.m[h] == NEG) ? 0.f : fmaxf(f, kLeastWeight);
     const float lf = st.l[h] * f;
     const float l = row_stride_sum<LPT>(swap_halves16(swap_halves32(lf, lf), swap_halves32(lf, lf)));
     // sixteen channel sums over the lane-groups: every exchange between rows halves the values a
@@ -575,11 +576,11 @@ __device__ __forceinline__ float shown_maximum(float m, float l) { return l == l
 // output) then counts the prefix in without knowing of it.  Weights of a pair (m, m') relative to the larger one:
 __device__ __forceinline__ float join_weights(float m, float mp, float &own, float &other) {
   const float mn = fmaxf(m, mp);
-  own = m > -INFINITY ? exp_nonpos_or_nan(m - mn) : 0.f;
-  other = mp > -INFINITY ? exp_nonpos_or_nan(mp - mn) : 0.f;
+  own = m > -INFINITY ? fmaxf(exp_nonpos_or_nan(m - mn), kLeastWeight) : 0.f;
+  other = mp > -INFINITY ? fmaxf(exp_nonpos_or_nan(mp - mn), kLeastWeight) : 0.f;
   return mn;
 }
-// x * w + y * v, where a weight of zero silences whatever its factor holds
+// x * w + y * v, where a weight of zero -- that of a result without slots -- silences whatever its factor holds
 __device__ __forceinline__ float join_values(float x, float w, float y, float v) {
   const float a = w == 0.f ? 0.f : x * w;
   return v == 0.f ? a : fmaf(y, v, a);
@@ -670,7 +671,7 @@ __device__ __forceinline__ void request_ema(const CacheView &cv, const Slice &sl
 }
 
 // ---------------------------------------------------------------------------------------
-// Epilogue shared by both bodies.  On entry wm/wl/wo hold NP per-wavefront partials
+// Epilogue shared by both bodies (kShared: with a shared prefix's partial results among the wavefronts').  On entry wm/wl/wo hold NP per-wavefront partials
 // (after a workgroup barrier): partial k is [G][D] floats, rows DS apart, at
 // wo + (k % kAttWaves) * WSTR + (k / kAttWaves) * G * DS; stash holds the slice's raw scores.
 // kPhase 0: the whole epilogue in one kernel (merge, publish, wait for the unit's other splits,
@@ -678,7 +679,7 @@ __device__ __forceinline__ void request_ema(const CacheView &cv, const Slice &sl
 // later launch, which needs no wait (wm/wl are unused and wo holds the [G][gs] weights) --
 // the pair serves shapes whose splits cannot all be resident at once.
 // ---------------------------------------------------------------------------------------
-template <int D, int G, int NP, int WSTR, int kPhase = 0, int DR = D, int DS = D, bool kPaged = false>
+template <int D, int G, int NP, int WSTR, int kPhase = 0, int DR = D, int DS = D, bool kPaged = false, bool kShared = false>
 __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const AttendLaunch &a,
                                                 const Slice &sl, int ns, int S, float *stash,
                                                 float *wm, float *wl, float *wo, float *gm,
@@ -714,6 +715,7 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
       row_m[b] = group_max(mk, 8);
       const bool live = mk > NEG;                      // an empty partial may hold anything and weighs nothing
       part_w[b] = live ? __expf(mk - row_m[b]) : 0.f;
+      if constexpr (kShared) part_w[b] = live ? fmaxf(part_w[b], kLeastWeight) : 0.f;
       row_l[b] = group_sum(live ? lk * part_w[b] : 0.f, 8);
     }
     // the statistics go out first: their trip to the unit's other splits runs behind the output merge
@@ -845,7 +847,8 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
       const float ms = mine ? __uint_as_float((unsigned)wvm) : NEG;
       const float ls = mine ? __uint_as_float((unsigned)wvl) : 0.f;
       const float M = group_max(ms, gs);
-      const float es = ms > NEG ? exp_nonpos(ms - M) : 0.f;          // an empty partial weighs nothing
+      const float least = kShared || (kPhase == 2 && a.shared_parts > 0) ? kLeastWeight : 0.f;
+      const float es = ms > NEG ? fmaxf(exp_nonpos(ms - M), least) : 0.f;   // an empty partial weighs nothing
       const double inv = recip_pos(group_sum((double)es * (double)ls, gs));
       if (mine) {
         if (os == 0) { gm[h] = M; ginv[h] = inv; ginv[G + h] = inv * row_weight<G>(a, h); }
@@ -1043,9 +1046,9 @@ __global__ __launch_bounds__(kAttThreads) void attend_kernel(const int32_t *w_le
   }
   stream_fp16_valu<D, G>(cv, a, sl, a.sm_scale, qf, st, stash, S);
   if constexpr (kShared) take_shared_valu<D, G>(a, sl, ns, st);
-  store_stream_partial<D, G>(st, threadIdx.x >> 6, wm, wl, wo + (threadIdx.x >> 6) * G * D);
+  store_stream_partial<D, G, kShared>(st, threadIdx.x >> 6, wm, wl, wo + (threadIdx.x >> 6) * G * D);
   __syncthreads();
-  attend_epilogue<D, G, NP, G * D, kSpill ? 1 : 0>(cv, a, sl, ns, S, stash, wm, wl, wo, gm, ginv, ema_old);
+  attend_epilogue<D, G, NP, G * D, kSpill ? 1 : 0, D, D, false, kShared>(cv, a, sl, ns, S, stash, wm, wl, wo, gm, ginv, ema_old);
 }
 
 // Second launch of the two-launch form: same grid; merges the published partials of the unit,
@@ -1847,7 +1850,7 @@ void attend_mfma_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t
   TS(17);
   __syncthreads();
   TS(18);
-  attend_epilogue<D, G, NP, kTileBytes / 4, kSpill ? 1 : 0, DR, kPartRow, kPaged>(cv, a, sl, ns, SS, stash, wm, wl, wo, gm, ginv, ema_old);
+  attend_epilogue<D, G, NP, kTileBytes / 4, kSpill ? 1 : 0, DR, kPartRow, kPaged, kShared>(cv, a, sl, ns, SS, stash, wm, wl, wo, gm, ginv, ema_old);
   TS_DUMP();
 }
 

@@ -84,9 +84,9 @@ struct SharedRowsState {
     l = 0.f;
   }
 
-  // The tile of keys key0 .. key0 + 31 at Kt, Vt.  bad: values that are no numbers were taken out of it (see drop_nonfinite).
+  // The tile of keys key0 .. key0 + 31 at Kt, Vt.
   template <int KROW, int VROW>
-  __device__ __forceinline__ void take(const uint8_t *Kt, const uint8_t *Vt, int key0, bool bad, const __half *V, int T, float sm) {
+  __device__ __forceinline__ void take(const uint8_t *Kt, const uint8_t *Vt, int key0, float sm) {
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5, t16 = lane & 15, c2 = (lane >> 4) & 1;
     const float NEG = -INFINITY, c = sm * 1.44269504088896341f;
     constexpr float kSlack = 4.0f, kLift = 10.0f;
@@ -136,17 +136,42 @@ struct SharedRowsState {
         O[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pb[s], O[nt], 0, 0, 0);
       }
     }
-    if (__builtin_expect(bad, 0)) {
-#pragma unroll 1
-      for (int key = key0; key < min(key0 + kShKeys, T); ++key) {
+  }
+
+  // Whether some channel is no number although the row's sum l, of both halves, is one.
+  __device__ __forceinline__ bool odd() const {
+    float z[8] = {};
 #pragma unroll
-        for (int nt = 0; nt < D / 32; ++nt)
+    for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i & 7] = fmaf(O[nt][i], 0.f, z[i & 7]);
+    const float all = ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
+    return all != all && l == l;
+  }
+
+  // Values that are infinite or NaN, of the keys of `tiles` (which calls its argument with the first key of each) that the lane's row
+  // sees: each makes its channel what they add up to, since a probability is positive however far the products above rounded it
+  // (where to zero, they made NaN of an infinite value, and where the values left the tile they were never met).
+  template <typename Tiles>
+  __device__ void show_odd_values(const __half *V, int T, Tiles tiles) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int nt = 0; nt < D / 32; ++nt) {
+      float sum[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+      tiles([&](int key0) {
+#pragma unroll 1
+        for (int key = key0; key < min(key0 + kShKeys, T); ++key) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float v = __half2float(V[(size_t)key * D + 32 * nt + 8 * (i / 4) + 4 * h + (i & 3)]);
-            if (key < lim && !(fabsf(v) < INFINITY)) O[nt][i] += v;
+            if (key < lim && !(fabsf(v) < INFINITY)) sum[i] += v;
           }
-      }
+        }
+      });
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[nt][i] = sum[i] == 0.f ? O[nt][i] : sum[i];
     }
   }
 };
@@ -237,7 +262,7 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
   if constexpr (RW == 1) all_least = st.least;
   st.reset();
   // Registers -> LDS.  Keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN
-  // value: where there are such rows these values leave the tile here and reach the rows that do see them later.
+  // value: where there are such rows these values leave the tile here and reach the rows that do see them at the end.
   auto store = [&](Turn &x, uint8_t *Kt, uint8_t *Vt, int base) {
     bool bad = false;
     if (base + kRowsLoaded > all_least) {
@@ -268,13 +293,14 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
     const int nn = (block * RW + p) * kShRows + (tid >> 4), bb = nn / a.unit_rows;
     out_at[p] = nn < rows ? ((bb * a.Hkv + g) * a.parts + part) * a.unit_rows + (nn - bb * a.unit_rows) : -1;
   }
+  bool dropped = false;                                  // values left a tile that was taken
   if constexpr (RW == 1) {
     uint8_t *Kt = s_tile + w * kShKeys * (L::KROW + L::VROW), *Vt = Kt + kShKeys * L::KROW;
     for (int key0 = first; key0 < min(hi, st.most); key0 += TK) {
-      const bool bad = __builtin_amdgcn_ballot_w64(store(x, Kt, Vt, key0)) != 0ull;
+      dropped |= store(x, Kt, Vt, key0);
       sh_wave_sync();
       if (key0 + TK < hi) load(x, key0 + TK);
-      st.template take<L::KROW, L::VROW>(Kt, Vt, key0, bad, V, a.T, a.sm_scale);
+      st.template take<L::KROW, L::VROW>(Kt, Vt, key0, a.sm_scale);
       sh_wave_sync();
     }
   } else {
@@ -290,12 +316,12 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
       if (base + TK < hi) fill(next, turn + 1, base + TK);
       if (base + 3 * TK < hi) load(next, base + 3 * TK);
       const uint8_t *Kt = buffer(turn), *Vt = Kt + TK * L::KROW;
-      const bool bad = s_bad[turn & 1] == turn;
+      dropped |= s_bad[turn & 1] == turn;
 #pragma unroll
       for (int sub = 0; sub < L::SUB; ++sub) {
         const int ks = (kw + L::KW * sub) * kShKeys;
         if (base + ks < min(hi, st.most))
-          st.template take<L::KROW, L::VROW>(Kt + ks * L::KROW, Vt + ks * L::VROW, base + ks, bad, V, a.T, a.sm_scale);
+          st.template take<L::KROW, L::VROW>(Kt + ks * L::KROW, Vt + ks * L::VROW, base + ks, a.sm_scale);
       }
       __syncthreads();
     };
@@ -309,6 +335,18 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
     }
   }
   st.l = (st.l + other_half(st.l)) * kUnlift;
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(dropped || st.odd()) != 0ull, 0)) {
+    st.show_odd_values(V, a.T, [&](auto take) {          // the wavefront's tiles, as above
+      const int end = min(hi, st.most);
+      if constexpr (RW == 1) {
+        for (int key0 = first; key0 < end; key0 += TK) take(key0);
+      } else {
+        for (int base = lo; base < hi; base += TK)
+          for (int sub = 0; sub < L::SUB; ++sub)
+            if (base + (kw + L::KW * sub) * kShKeys < end) take(base + (kw + L::KW * sub) * kShKeys);
+      }
+    });
+  }
   // (-inf stays; a sum that is NaN, from a score that is none, outweighs the others: a merge shall not lose it to larger scores)
   if (h == 0) {
     s_m[w][l32] = st.l == st.l ? st.mref * a.sm_scale : INFINITY;
@@ -337,7 +375,7 @@ __global__ __launch_bounds__(kShThreads) __attribute__((amdgpu_waves_per_eu(2, 2
     }
 #pragma unroll
     for (int k = 0; k < L::KW; ++k) {
-      m[k] = m[k] == NEG ? 0.f : __expf(m[k] - M);       // (a wavefront that saw no key of the row: its partial is zero)
+      m[k] = m[k] == NEG ? 0.f : fmaxf(__expf(m[k] - M), kLeastWeight);   // (a wavefront that saw no key of the row: its partial is zero)
       sum = fmaf(m[k], s_l[p + k * RW][row], sum);
     }
     if ((tid & 15) == 0) a.ml[out_at[p]] = make_float2(M, sum);

@@ -10,6 +10,10 @@ namespace confkv {
 
 constexpr int kWave = 64;
 constexpr int kMaxLayers = 256;
+// Least weight of a partial result that holds keys, where a shared prefix's are merged: nothing beside a finite one, whose share of
+// the result is 2^-60 at most, while one that is infinite or NaN, from a value that is, stays so (0 x inf would be NaN, and leaving
+// weights of zero out would lose it).
+constexpr float kLeastWeight = 0x1p-90f;
 
 // Indices into the device statistics block (unsigned long long each).
 enum StatSlot { kStatEvicted = 0, kStatDemoted = 1, kStatTight = 2, kStatLoose = 3,

@@ -125,3 +125,35 @@ def test_own_key_not_a_number_behind_a_larger_prefix(lib, torch_cuda, monkeypatc
         got = _out(c, True, q, kn, vn)
         assert np.isnan(got[1]).all() and np.isfinite(got[0]).all(), T
         c.close()
+
+
+@pytest.mark.parametrize("splits,two_launch", _LAUNCHES)
+@pytest.mark.parametrize("row_waves", [1, 2, 4])
+@pytest.mark.parametrize("lead", [0.0, 20.0, 40.0, 200.0])
+@pytest.mark.parametrize("D,G,tq", _FORMS)
+def test_odd_prefix_values_of_any_weight(lib, torch_cuda, monkeypatch, D, G, tq, lead, row_waves, splits, two_launch):
+    """Values that are infinite or NaN, with a probability of e^-lead beside one key of the prefix or of the cache: what the
+    sequences that see them get is the same whether the others see them or not."""
+    B, T, at = 3, 1500, (3, 700, 701, 1499)
+    for where in ("prefix", "own"):
+        for seen in (None, [T, T, 2], [T, 702, 1490]):
+            c = _Case(lib, torch_cuda, monkeypatch, D, G, 1, B, T, 40, -1, tq=tq, splits=splits, two_launch=two_launch, row_waves=row_waves,
+                      seen=seen)
+            q, kn, vn = _leading(c, lead, where, 1)
+            odd = ((at[0], 0, math.inf), (at[1], 9, -math.inf), (at[1], D - 1, math.nan), (at[2], 33, math.inf), (at[2], 9, -math.inf),
+                   (at[3], 33, -math.inf), (at[3], 50, math.inf))
+            for t, d, x in odd:
+                c.pv[0, t, d] = x
+            _share(c)
+            got = _out(c, True, q, kn, vn)
+            for b in range(B):
+                ref = [0.0] * D
+                for t, d, x in odd:
+                    if t < (T if seen is None else seen[b]):
+                        ref[d] += x                           # (infinities that meet: NaN)
+                ref = np.array(ref)
+                fine = ref == 0
+                assert np.isfinite(got[b][..., fine]).all(), (where, seen, b)
+                shown = np.broadcast_to(ref[~fine], got[b][..., ~fine].shape)
+                assert np.array_equal(got[b][..., ~fine], shown, equal_nan=True), (where, seen, b, got[b][0, 0, ~fine], ref[~fine])
+            c.close()
