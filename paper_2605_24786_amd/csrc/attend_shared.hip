@@ -117,13 +117,13 @@ struct SharedRowsState {
       for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
     }
     // Probabilities are held 2^10 times as large, at most 55910 of fp16's 65504: as fp16 operands they keep eleven bits down to
-    // 6e-8 (unscaled 6e-5, which the tail of a long prefix is below).  (The rounding of mref * c is the same for all keys of
-    // the row: it only scales m, by less than the scores' own rounding.)
-    const float ref = (mref == NEG ? 0.f : mref * c) - kLift;
+    // 6e-8 (unscaled 6e-5, which the tail of a long prefix is below).  (The difference comes first: a rounded mref * c is off by
+    // more than fp16's exponents from scores of 10^7 on.)
+    const float ref = mref == NEG ? 0.f : mref;
     sh_h8 pb[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -ref));
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[i] - ref, c, kLift));
       l += p;
       pb[i / 8][i & 7] = (_Float16)p;                  // (fp16 operands: half a step, 2^-11 of each probability)
     }

@@ -391,3 +391,27 @@ def test_refusals(lib, torch_cuda, monkeypatch):
     with pytest.raises(lib.ConfKVError):
         none.attend_shared(0, z(1, 8), z(1, 2), z(1, 2), z(1, 8), pk, pv)
     none.close()
+
+
+@pytest.mark.parametrize("row_waves", [1, 2, 4])
+@pytest.mark.parametrize("D,G,tq", [(128, 4, 1), (64, 1, 1), (128, 4, 3)])
+@pytest.mark.parametrize("size", [1000.0, 9000.0, 60000.0])
+def test_largest_scores(lib, torch_cuda, monkeypatch, size, D, G, tq, row_waves):
+    """Queries and keys as large as FP16 holds: scores of 5e6 to 4e10, of which one key has the largest by more than any rounding.
+    What it leaves to the others is nothing, and its probability is one."""
+    torch = torch_cuda
+    T = 1300
+    c = _Case(lib, torch, monkeypatch, D, G, 1, 4, T, 40, -1, tq=tq, seed=int(size), row_waves=row_waves)
+    for win in (0, 31, 700, T - 1):
+        q, kn, vn = c.inputs()
+        q[:] = size
+        c.pk[:] = (c.rng.random((1, T, D)) * 0.5 * size).astype(np.float16)      # a quarter of the largest score, more or less
+        c.pk[0, win] = size * (0.9 + 0.1 * c.rng.random())
+        c.shared[0].copy_(c.on(c.pk))
+        out = torch.full((4, tq, G, D), math.nan, dtype=torch.float16, device="cuda")
+        c.kv.attend_shared(0, c.on(q), c.on(kn), c.on(vn), out, *c.shared)
+        got = out.cpu().numpy()
+        assert np.array_equal(got, np.broadcast_to(c.pv[0, win], got.shape)), win
+        c.kv.evict_compact()
+        assert all(np.isfinite(c.kv.export(0, b, 0)["ema"]).all() for b in range(4))
+    c.close()
