@@ -14,12 +14,15 @@
 // and written, more than a large copy reaches); where a line is met by two accesses they cost (64 channels of float32, 32 of
 // them turning, 5271 tokens: 162 and 200 us), so these, and short calls, whose result is read next, do without.
 // A decode step's call is a launch (3 to 4 us on the device): its rows are spread over as many wavefronts as they make.
+#include <algorithm>
+
 #include "confkv_dev.h"
 #include "launch.h"
 
 namespace confkv {
 
 constexpr int kPrepWaves = 4;
+constexpr int kPrepGridX = 1 << 23;                    // workgroups along x: a dimension of a grid has fewer than 2^32 threads
 
 typedef _Float16 prep_h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 prep_h8 __attribute__((ext_vector_type(8)));
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaun
   constexpr int kRun = kType == kTypeFp32 ? 4 : 8, kSets = 8 / kRun;   // a lane's sets of two runs
   __shared__ float2 s_turn[kPrepWaves][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long task = (long long)blockIdx.x * kPrepWaves + w;
+  const long long task = ((long long)blockIdx.y * kPrepGridX + blockIdx.x) * kPrepWaves + w;
   const long long tok = task / parts;
   if (tok >= (long long)a.B * a.tokens) return;
   const int part = (int)(task - tok * parts);
@@ -200,13 +203,13 @@ hipError_t launch_prepare(const PrepareLaunch &a, int D, int type, hipStream_t s
   while (per > 1 && tokens * ((passes + per - 1) / per) < 4096) per = (per + 1) / 2;
   const int parts = (passes + per - 1) / per;
   const long long blocks = (tokens * parts + kPrepWaves - 1) / kPrepWaves;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)std::min<long long>(blocks, kPrepGridX), (unsigned)((blocks + kPrepGridX - 1) / kPrepGridX));
   // (see the top)
   const bool stream_lines = D == 128 && type != kTypeFp32 && (a.interleaved || a.rotated == 0 || a.rotated == D) && tokens >= 4096;
   auto fn = type == kTypeFp32 ? (D == 64 ? prepare_kernel<kTypeFp32, 64, false> : prepare_kernel<kTypeFp32, 128, false>)
           : type == kTypeFp16 ? (D == 64 ? prepare_kernel<kTypeFp16, 64, false> : stream_lines ? prepare_kernel<kTypeFp16, 128, true> : prepare_kernel<kTypeFp16, 128, false>)
                               : (D == 64 ? prepare_kernel<kTypeBf16, 64, false> : stream_lines ? prepare_kernel<kTypeBf16, 128, true> : prepare_kernel<kTypeBf16, 128, false>);
-  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(kPrepWaves * kWave), 0, stream, a, parts, per);
+  hipLaunchKernelGGL(fn, grid, dim3(kPrepWaves * kWave), 0, stream, a, parts, per);
   return hipGetLastError();
 }
 

@@ -219,3 +219,22 @@ def test_destinations_that_overlap_are_refused(lib, torch_cuda):
     for i, x in ((2 * n, q), (0, k), (n, v)):
         assert torch.equal(at(i), x)
     kv.close()
+
+
+def test_more_tokens_than_a_grid_dimension(lib, torch_cuda):
+    """2^26 + 13 tokens, one wavefront each: more threads than one dimension of a launch has.  Every token reads the same row; keys at
+    the handle's positions, sampled, and all values."""
+    torch = torch_cuda
+    T, D = 2 ** 26 + 13, 64
+    kv = _kv(lib, 1, 1, 1, D)
+    row = torch.randn(2, D, generator=torch.Generator().manual_seed(6)).half().cuda()
+    k, v = (r.view(1, 1, 1, D).expand(1, T, 1, D) for r in row)
+    freq = (100.0 ** (-torch.arange(32) / 32.0)).float().cuda()
+    k16, v16 = (torch.zeros(1, T, 1, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    kv.prepare_qkv(0, None, k, v, k16=k16, v16=v16, freq=freq)
+    torch.cuda.synchronize()
+    for part in v16.view(T, D).split(2 ** 23):
+        assert bool((part == row[1]).all())
+    at = torch.tensor([0, 1, 2 ** 23 * 4 - 1, 2 ** 23 * 4, 2 ** 25 + 5, 2 ** 26 - 1, 2 ** 26, T - 2, T - 1])
+    _close(torch, k16[:, at.cuda()], *_reference(torch, k[:, at.cuda()], None, freq, at[None].int(), False, 0.0), "keys")
+    kv.close()
