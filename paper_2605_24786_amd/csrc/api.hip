@@ -638,6 +638,7 @@ int conf_kv_prepare_qkv(conf_kv_handle *h, int32_t layer, const conf_kv_qkv *arg
   a.pos = q.dev_pos;
   a.next = h->cv.ctl + kCtlPos + layer;
   a.first = q.first;
+  if (!q.dev_pos) a.first += h->appended[layer];                      // (the device's position moves on with the eviction)
   a.q16 = (__half *)q.dev_q16;
   a.k16 = (__half *)q.dev_k16;
   a.v16 = (__half *)q.dev_v16;

@@ -42,7 +42,7 @@ struct PrepareLaunch {
   const float *wq, *wk, *freq;           // norm weights (null: no norm), angles per position
   const int32_t *pos;                    // [B][tokens], or null: *next + token
   const unsigned *next;
-  long long first;                       // added to every position
+  long long first;                       // added to every position (and, without pos, what a call has appended since the last eviction)
   __half *q16, *k16, *v16;
   int B, tokens, Hq, Hkv;
   int rotated, interleaved, prompt;

@@ -238,3 +238,48 @@ def test_more_tokens_than_a_grid_dimension(lib, torch_cuda):
     at = torch.tensor([0, 1, 2 ** 23 * 4 - 1, 2 ** 23 * 4, 2 ** 25 + 5, 2 ** 26 - 1, 2 ** 26, T - 2, T - 1])
     _close(torch, k16[:, at.cuda()], *_reference(torch, k[:, at.cuda()], None, freq, at[None].int(), False, 0.0), "keys")
     kv.close()
+
+
+@pytest.mark.parametrize("c", [1, 3])
+def test_positions_of_the_handle_behind_an_append(lib, torch_cuda, c):
+    """Between the attention, which appends, and conf_kv_evict_compact, which ends the step, the next appended token is the one behind
+    the call's own -- recorded as well."""
+    torch = torch_cuda
+    B, Hq, Hkv, D, T, T0 = 2, 8, 2, 128, 2, 11
+    g = torch.Generator().manual_seed(5)
+    kv = _kv(lib, B, Hq, Hkv, D, max_chunk=4)
+    for layer in (0, 1):
+        kv.load_prefill(layer, *(torch.randn(B, Hkv, T0, D, generator=g).half().cuda() for _ in range(2)))
+    q = torch.randn(B, T, Hq, D, generator=g).half().cuda()
+    freq = (100.0 ** (-torch.arange(64) / 64.0)).float().cuda()
+    q16, before, behind, other, ref = (torch.zeros_like(q) for _ in range(5))
+    new = [torch.randn(B, c, h, D, generator=g).half().cuda() for h in (Hq, Hkv, Hkv)]
+    out = torch.empty_like(new[0])
+
+    def calls():
+        kv.prepare_qkv(0, q, None, None, before, freq=freq, first=7)
+        kv.attend_chunk(0, *new, out)
+        kv.prepare_qkv(0, q, None, None, behind, freq=freq, first=7)
+        kv.prepare_qkv(1, q, None, None, other, freq=freq, first=7)
+        kv.attend_chunk(1, *new, out)
+        kv.evict_compact()
+
+    def check(steps):
+        torch.cuda.synchronize()
+        at = T0 + c * steps
+        for got, start in ((before, at), (behind, at + c), (other, at)):
+            pos = (start + 7 + torch.arange(T, dtype=torch.int32)).repeat(B, 1).cuda()
+            kv.prepare_qkv(0, q, None, None, ref, freq=freq, pos=pos)
+            torch.cuda.synchronize()
+            assert torch.equal(got, ref), steps
+
+    kv.static_plan(True)
+    calls()
+    check(0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for i in range(1, 5):
+        graph.replay()
+        check(i)
+    kv.close()
