@@ -412,8 +412,8 @@ typedef struct conf_kv_qkv {
  * layout) take, in one pass.  Each query and key head x of a token becomes
  *     y = x / sqrt(mean(x^2) + eps) * weight           (where a weight is given, else y = x)
  *     (a, b) <- (a cos t - b sin t, b cos t + a sin t) for the pairs of its first `rotated` channels, t = position * freq
- * and is rounded to fp16 once; values are rounded to fp16.  Angles are formed in float64, norms and products in float32.  What
- * is beyond fp16's range becomes infinite.  Each of q, k and v may be left out (source and destination NULL), not all.
+ * and is rounded to fp16 once; values are rounded to fp16.  Angles are formed in float64, norms (of rows of any size) and products
+ * in float32.  What is beyond fp16's range becomes infinite.  Each of q, k and v may be left out (source and destination NULL), not all.
  * The handle gives B, Hq, Hkv, D and, with dev_pos NULL, the positions, which live on the device: a recorded call moves on
  * with the cache.  Nothing of the cache changes.  Tensors are 16-byte aligned and so are the strides in bytes; destinations lie
  * apart from each other and from the sources (what is between a source's first and last value).  B * T at most 2^30. */

@@ -145,16 +145,35 @@ __global__ __launch_bounds__(kPrepWaves * kWave) void prepare_kernel(PrepareLaun
       for (int i = 0; i < 2; ++i) unpack_run<kType, kRun>(raw[s][i], f[s][i]);
     const float *wt = kind == 0 ? a.wq : kind == 1 ? a.wk : nullptr;
     if (wt) {
-      float ss = 0.f;
+      auto sum_of_squares = [&]() {
+        float ss = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSets; ++s)
+        for (int s = 0; s < kSets; ++s)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < kRun; ++e) ss = fmaf(f[s][i][e], f[s][i][e], ss);
+            for (int e = 0; e < kRun; ++e) ss = fmaf(f[s][i][e], f[s][i][e], ss);
 #pragma unroll
-      for (int m = LPR / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, kWave);
-      const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+        for (int m = LPR / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, kWave);
+        return ss;
+      };
+      float ss = sum_of_squares(), eps = a.eps;
+      // A row whose squares leave float32 (FP16's do not) is scaled by a power of two, its norm's eps by its square.
+      if constexpr (kType != kTypeFp16) {
+        const bool large = !(ss < 3e38f), small = ss < 1e-30f && eps < 1e-30f;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(large || small) != 0ull, 0)) {
+          const float by = large ? 0x1p-70f : small ? 0x1p100f : 1.f;
+#pragma unroll
+          for (int s = 0; s < kSets; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < kRun; ++e) f[s][i][e] *= by;
+          ss = sum_of_squares();
+          eps = eps * by * by;
+        }
+      }
+      const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
 #pragma unroll
       for (int s = 0; s < kSets; ++s)
 #pragma unroll

@@ -283,3 +283,31 @@ def test_positions_of_the_handle_behind_an_append(lib, torch_cuda, c):
         graph.replay()
         check(i)
     kv.close()
+
+
+@pytest.mark.parametrize("D,interleaved", [(128, False), (64, True)])
+@pytest.mark.parametrize("dtype,scale", [("float32", 1e25), ("float32", 3e37), ("float32", 1e-30), ("float32", 1e-38), ("bfloat16", 1e30),
+                                         ("bfloat16", 1e-25), ("float16", 2e-7), ("float16", 1.2e4)])
+def test_norm_of_rows_whose_squares_leave_float32(lib, torch_cuda, dtype, scale, D, interleaved):
+    """Rows so large or small that the sum of their squares is no float32 number, beside ordinary ones and one of zeros: what the norm
+    makes of them is of the size of its weight (eps: 0 for the small ones, which it would drown)."""
+    torch = torch_cuda
+    B, T, Hq, Hkv = 1, 3, 6, 2
+    g = torch.Generator().manual_seed(9)
+    size = torch.tensor([scale, 1.0, 1.0, scale, 1.0, scale])[:, None]
+    q = (torch.randn(B, T, Hq, D, generator=g).clamp(-5, 5) * size).to(getattr(torch, dtype)).cuda()
+    k = (torch.randn(B, T, Hkv, D, generator=g).clamp(-5, 5) * scale).to(getattr(torch, dtype)).cuda()
+    eps = 1e-5 if scale > 1 else 0.0
+    if eps:
+        q[0, 1, 4] = 0
+    w = (1 + 0.3 * torch.randn(2, D, generator=g)).cuda()
+    freq = (100.0 ** (-torch.arange(D // 2) / (D / 2))).float().cuda()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[None]
+    kv = _kv(lib, B, Hq, Hkv, D)
+    q16 = torch.empty(B, T, Hq, D, dtype=torch.float16, device="cuda")
+    k16 = torch.empty(B, T, Hkv, D, dtype=torch.float16, device="cuda")
+    kv.prepare_qkv(0, q, k, None, q16, k16, freq=freq, pos=pos, q_weight=w[0], k_weight=w[1], eps=eps, interleaved=interleaved)
+    torch.cuda.synchronize()
+    _close(torch, q16, *_reference(torch, q, w[0], freq, pos, interleaved, eps), "queries")
+    _close(torch, k16, *_reference(torch, k, w[1], freq, pos, interleaved, eps), "keys")
+    kv.close()
