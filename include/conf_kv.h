@@ -298,7 +298,9 @@ typedef struct conf_kv_prefix {
  * and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend); tq * n_q_heads / n_kv_heads at most 16, and more than
  * max_shared tokens, a null or misaligned prefix are CONF_KV_ERR_INVALID_ARG.  Prefix tensors are 16-byte aligned.
  * Positions are the caller's affair: the handle's count the cache only (conf_kv_prepare_qkv's `first` adds the prefix).
- * conf_kv_observe* see the cache alone.  A recorded call keeps the prefix's place and length and reads dev_seen anew. */
+ * conf_kv_observe* see the cache alone: the importance they give sums to G per query, that of a step behind a prefix to G minus
+ * the prefix's share, so slots that carry both stand higher than a step would put them until the average has moved on (a lower
+ * start can be handed to conf_kv_load_prefill instead).  A recorded call keeps the prefix's place and length and reads dev_seen anew. */
 int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const conf_kv_prefix *prefix, const void *dev_q16,
                           const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream);
 

@@ -151,27 +151,39 @@ struct SharedRowsState {
 
   // Values that are infinite or NaN, of the keys of `tiles` (which calls its argument with the first key of each) that the lane's row
   // sees: each makes its channel what they add up to, since a probability is positive however far the products above rounded it
-  // (where to zero, they made NaN of an infinite value, and where the values left the tile they were never met).
+  // (where to zero, they made NaN of an infinite value, and where the values left the tile they were never met).  The first
+  // pass empties these channels, the second adds; tiles without such a value cost a read.
   template <typename Tiles>
-  __device__ void show_odd_values(const __half *V, int T, Tiles tiles) {
-    const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll
-    for (int nt = 0; nt < D / 32; ++nt) {
-      float sum[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-      tiles([&](int key0) {
+  __device__ __forceinline__ void show_odd_values(const __half *V, int T, Tiles tiles) {
+    constexpr int PR = D / 8;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll 1
-        for (int key = key0; key < min(key0 + kShKeys, T); ++key) {
+    for (int pass = 0; pass < 2; ++pass) {
+      tiles([&](int key0) {
+        const int end = min(key0 + kShKeys, T);
+        unsigned any = 0u;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float v = __half2float(V[(size_t)key * D + 32 * nt + 8 * (i / 4) + 4 * h + (i & 3)]);
-            if (key < lim && !(fabsf(v) < INFINITY)) sum[i] += v;
-          }
+        for (int j = 0; j < kShKeys * PR / kWave; ++j) {
+          const int4 v = *(const int4 *)(V + (size_t)min(key0 + (lane + j * kWave) / PR, T - 1) * D + lane % PR * 8);
+          any |= nonfinite_halfs(v.x) | nonfinite_halfs(v.y) | nonfinite_halfs(v.z) | nonfinite_halfs(v.w);
+        }
+        if (__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0u) == 0ull) return;
+#pragma unroll 1
+        for (int key = key0; key < end; ++key) {
+          sh_h4 v[D / 32][4];
+#pragma unroll
+          for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[nt][k] = *(const sh_h4 *)(V + (size_t)key * D + 32 * nt + 8 * k + 4 * h);
+#pragma unroll
+          for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = (float)v[nt][i / 4][i & 3];
+              if (key < lim && !(fabsf(x) < INFINITY)) O[nt][i] = pass ? O[nt][i] + x : 0.f;
+            }
         }
       });
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[nt][i] = sum[i] == 0.f ? O[nt][i] : sum[i];
     }
   }
 };
