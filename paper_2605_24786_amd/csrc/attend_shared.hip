@@ -3,9 +3,9 @@
 //
 // All rows (sequence, token, head of the group) of a kv-head meet every prefix key, so this is a product of [rows x D] with
 // [D x T] and, behind the softmax, of [rows x T] with [T x D]: matrix instructions on tiles that the whole batch shares.  The
-// prefix is cut into `parts`; a workgroup takes one part for 32 rows of a kv-head, and its eight wavefronts take the part's tiles
-// of 32 keys in turn, each keeping the running maximum, sum and output of the rows (online softmax).  They merge at the end and
-// leave float32:
+// prefix is cut into `parts`; a workgroup takes one part for 32, 64 or 128 rows of a kv-head, and its eight wavefronts take the
+// part's tiles of 32 keys in turn, each keeping the running maximum, sum and output of 32 rows (online softmax).  They merge at the
+// end and leave float32:
 //   ml[unit][part][row] = (m, l),  o[unit][part][row][D] = sum over the part's keys of e^(s - m) v
 // The products are formed transposed, scores [32 keys x 32 rows] and output [D x 32 rows]: a lane then holds values of one row
 // only, its probabilities are the operand of the second product as they stand, and the row's statistics need one exchange
@@ -125,7 +125,10 @@ struct SharedRowsState {
     for (int i = 0; i < 16; ++i) {
       const float p = __builtin_amdgcn_exp2f(fmaf(sc[i] - ref, c, kLift));
       l += p;
-      pb[i / 8][i & 7] = (_Float16)p;                  // (fp16 operands: half a step, 2^-11 of each probability)
+      // (fp16 operands: half a step, 2^-11 of each probability.  32 sequences behind 4096 tokens are 2.3e-4 from a float64
+      // evaluation, relative, against 2.1e-4 of one that keeps float32 until it rounds the result; a second operand for what the
+      // rounding leaves would double the products.)
+      pb[i / 8][i & 7] = (_Float16)p;
     }
     const uint8_t *vp = Vt + (4 * h + (t16 >> 2)) * VROW + 32 * c2 + 8 * (t16 & 3);
 #pragma unroll
@@ -191,8 +194,9 @@ struct SharedRowsState {
 // Workgroups of one (kv-head, part) read the same keys for different rows, so they shall share an L2: workgroups go to the eight
 // XCDs in turn, and XCD x takes the logical ones x * each .. x * each + each - 1 (rows fastest, then parts, then kv-heads).
 //
-// What bounds it: the prefix's bytes, up to some 400 rows per kv-head; a short prefix the chain of a workgroup (first rows, a
-// tile or two, the merge).  With up to 32 rows (RW = 1) a wavefront waits for nobody before the merge: it loads and multiplies
+// What bounds it: the prefix's bytes for some forty rows per kv-head; with more of them what every row adds, products, exponentials and
+// reads of the tiles in LDS (80 rows behind 32001 tokens: 40 us, where the bytes take 25; at the rates of a large copy and a large
+// product bytes and operations meet at 220 rows); a short prefix the chain of a workgroup (first rows, a tile or two, the merge).  With up to 32 rows (RW = 1) a wavefront waits for nobody before the merge: it loads and multiplies
 // tiles of its own, the next one in flight in registers while this one is used.  More rows share a turn's tiles through LDS, two
 // buffers, one barrier per turn, the two turns after the next in flight.
 // Its loads are streaming ones although several workgroups may read a line: plain loads took 17.9 us instead of 12.7 (8192 tokens, 32
@@ -414,9 +418,10 @@ size_t shared_parts_most(int tokens) { return (size_t)std::min(kSharedMaxParts, 
 // as many too but where the partial results outweigh the prefix.
 // Rows side by side: `blocks` workgroups read the same keys, some 18 TB/s all together where an L2 serves most of them, so fewer
 // blocks save loads; each doubling of RW costs the barriers and a longer way to the first product and from the last, about 7 us'
-// worth of loads.  us per layer (prefix and cache of 256 tokens, 128 channels, 8 kv-heads) with RW = 1, 2, 4: 128 rows behind 4096
-// tokens 25.1, 26.2, 28.8, 12000 34.9, 33.5, 37.0, 32768 63.0, 49.9, 49.9; 40 rows, 12000 26.8, 29.1, 30.7, 32768 43.9, 40.5, 43.0; 256 rows,
-// 4096 29.9, 29.7, 31.0, 32768 96.2, 74.4, 66.0.
+// worth of loads.  us per layer (prefix and cache of 256 tokens, 128 channels, 8 kv-heads) with RW = 1, 2, 4: 40 rows behind 12000
+// tokens 27.5, 29.4, 30.9, 32768 45.5, 41.0, 43.0; 128 rows, 4096 25.2, 26.0, 29.4, 12000 35.8, 35.0, 38.1, 32768 65.3, 52.7, 56.1; 256 rows,
+// 4096 30.6, 29.9, 31.5, 12000 48.5, 43.5, 45.0, 32768 98.0, 77.3, 73.0.  (So the rule is off by up to 6 %: it takes 4 for 128 rows behind
+// 32768.)
 void shared_plan(int rows, int Hkv, int D, int T, int cus, int forced_row_waves, SharedPlan *p) {
   constexpr double kStep = 7e-6 * 18e12;
   double least = 0.0;

@@ -61,10 +61,11 @@ __device__ __forceinline__ void load_quad(const void *row, int i, float (&x)[4])
 // many rows it is the bytes of the logits and, with long histories, the vector ALU: every range passes over the row's whole
 // history, some seven instructions per token and wavefront.  So sixteen wavefronts share a pass, and a range is 4096 logits per
 // quad of a thread, with as many quads (1, 2, 4 or 5) as make the fewest rounds of workgroups over the CUs times their length.
-// us with 1, 2, 4, 5 quads (BF16 logits, 64 biases, a mask; histories of 300 and 32768 tokens): 8 rows of 128256 4.5, 5.1, 6.2, 6.8
-// and 6.9, 7.9, 9.7, 10.9; 32 of 50257 6.3, 6.0, 7.2, 7.8 and 9.8, 8.9, 11.1, 12.1; 32 of 152064 12.9, 11.0, 10.0, 9.7 and 19.3, 15.8, 15.5,
-// 13.7 (24 MB read and written, 4 more of history: 2.3 TB/s; without a history 8.1: 3.7).  256 threads of four quads: 1 row of
-// 128256 5.0 and 10.8 against 3.9 and 5.9.
+// us with 1, 2, 4, 5 quads (BF16 logits, 64 biases, a mask; histories of 300 and 32768 tokens): 8 rows of 128256 4.4, 4.9, 6.1, 6.6
+// and 6.8, 7.5, 9.5, 10.5; 32 of 50257 6.1, 5.8, 7.0, 7.5 and 9.9, 8.8, 10.9, 12.0; 32 of 152064 12.9, 11.0, 10.1, 9.8 and 19.1, 15.6, 15.5,
+// 13.6 (30 MB read and written, 3.6 more of history: 2.5 TB/s; without a history 8.3: 3.6).  Three quads, which are not among them, took
+// 9.4 and 14.0 there, and 6.9 and 10.5 for 32 rows of 85000, which have four (7.5 and 11.5).  256 threads of four quads: 1 row of
+// 128256 5.0 and 10.8 against 3.8 and 5.8.
 // Tried and slower: a row's blocks of 64 logits dealt out among its workgroups, which spreads the frequent low token numbers but
 // takes twice the instructions per token; one LDS operation for up to four tokens of a lane; more tokens in flight.
 // Rows are the grid's fast axis: with a multiple of eight of them all ranges of a row run on one XCD, whose L2 then serves the
