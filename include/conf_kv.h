@@ -294,7 +294,8 @@ typedef struct conf_kv_prefix {
  * cache and the call's own tokens up to themselves, in one softmax,
  *     out[b][t][h] = sum_i p_i V_i,   p = softmax over prefix and cache of sm_scale * q . K_i,
  * and the importance of the cached slots follows the probabilities of that softmax (what goes to the prefix goes to no slot:
- * sum_i A_i = G minus the prefix's share).  The prefix's keys and values are read once for the whole batch.  Tensors, errors
+ * sum_i A_i = G minus the prefix's share).  The prefix's keys and values are read once for the whole batch; one that is infinite
+ * or NaN shows in the sequences that see its token and in no other.  Tensors, errors
  * and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend); tq * n_q_heads / n_kv_heads at most 16, and more than
  * max_shared tokens, a null or misaligned prefix are CONF_KV_ERR_INVALID_ARG.  Prefix tensors are 16-byte aligned.
  * Positions are the caller's affair: the handle's count the cache only (conf_kv_prepare_qkv's `first` adds the prefix).
