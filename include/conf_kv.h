@@ -10,7 +10,8 @@
  *     once:             conf_kv_step            (confidence -> tight/loose budget)
  *     once:             conf_kv_evict_compact   (rank, evict, compact, demote)
  *
- * and, where a program wants them, conf_kv_prepare_qkv in front of the attention (projection rows ->
+ * and, where a program wants them, conf_kv_attend_pages and conf_kv_load_pages for a prompt that lies in pages,
+ * conf_kv_attend_diff for models with differential attention, conf_kv_prepare_qkv in front of the attention (projection rows ->
  * queries, keys, values), conf_kv_attend_shared in its place (a prefix that sequences share) and
  * conf_kv_constrain in front of conf_kv_step (penalties, biases, grammar masks).
  *
@@ -116,6 +117,8 @@ typedef struct conf_kv_config {
   int32_t layout;            /* conf_kv_layout: where the INT8 slots of a unit live              */
   int32_t max_shared;        /* most tokens of a shared prefix that conf_kv_attend_shared may be given (sizes the scratch
                                 buffer: up to 64 partial results per query row), up to 2^30; 0: none         */
+  int32_t max_paged;         /* most tokens of a sequence in the pages that conf_kv_attend_pages may be given (above 128: 256
+                                blocks of 128 partial results in the scratch buffer), up to 2^30; 0: none     */
 } conf_kv_config;
 
 typedef enum conf_kv_layout {
@@ -304,6 +307,57 @@ typedef struct conf_kv_prefix {
  * start can be handed to conf_kv_load_prefill instead).  A recorded call keeps the prefix's place and length and reads dev_seen anew. */
 int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const conf_kv_prefix *prefix, const void *dev_q16,
                           const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream);
+
+/* A paged FP16 cache of the caller's, in which prompts are kept while they are worked off: the rows of token t of sequence b
+ * lie in page table[b][t / page_tokens], slot t % page_tokens, kv-head g's at page * page_stride + slot * token_stride +
+ * g * head_stride (so a page may be [slots][Hkv][D] or [Hkv][slots][D], and keys and values may take turns).  Entries that a
+ * sequence's tokens do not reach are not used.  An entry outside 0 .. n_pages - 1 where a token is: its rows are
+ * taken from some page, and what would be written there is not written. */
+typedef struct conf_kv_pages {
+  void *dev_k16;             /* fp16, heads of D values, 16-byte aligned                                        */
+  void *dev_v16;             /* the same                                                                       */
+  int64_t page_stride, token_stride, head_stride;   /* in values, multiples of 8; rows do not overlap              */
+  int32_t page_tokens;       /* a power of two, 8 .. 2^20                                                      */
+  int32_t n_pages;           /* pages there are, 1 .. 2^30                                                     */
+  const int32_t *dev_table;  /* int32 [B][max_pages], rows table_stride entries apart                          */
+  int64_t table_stride;      /* >= max_pages                                                                   */
+  int32_t max_pages;         /* entries per sequence, >= 1; max_pages * page_tokens at most 2^30                */
+} conf_kv_pages;
+
+/* New tokens of every sequence: rows start .. start + new - 1 of the row tensors, behind `context` tokens that the pages hold. */
+typedef struct conf_kv_chunk {
+  int32_t tokens;            /* most new tokens of a sequence, >= 0                                             */
+  int32_t rows;              /* rows of the row tensors                                                        */
+  const int32_t *dev_starts; /* int32 [B]; NULL: b * tokens (rows >= B * tokens)                                */
+  const int32_t *dev_new;    /* int32 [B], held within 0 .. tokens, within the rows and within the pages' room;
+                                NULL: `tokens` each                                                            */
+  const int32_t *dev_context;/* int32 [B], held within 0 .. max_pages * page_tokens                             */
+  const void *dev_q16;       /* fp16 [rows][Hq][D]                                                             */
+  const void *dev_knew16;    /* fp16 [rows][Hkv][D], or NULL with dev_vnew16: the pages hold the new tokens too  */
+  const void *dev_vnew16;
+  void *dev_out16;           /* fp16 [rows][Hq][D], or [rows][Hq / 2][D] with dev_lambda; written               */
+  const float *dev_lambda;   /* fp32 [rows][Hq / 2], rows lambda_stride values apart, or NULL                   */
+  int64_t lambda_stride;     /* >= 0; 0: the same weights for every row                                        */
+} conf_kv_chunk;
+
+/*
+ * Attention of a chunk of new tokens over a paged cache, of any length per sequence: a prompt's chunks, single tokens and
+ * sequences without new tokens in one call.  New keys and values go to their pages (tokens context .. context + new - 1), and
+ *     out[start + t][h] = sum_i p_i V_i,   p = softmax over tokens i <= context + t of sm_scale * q . K_i
+ * with float32 accumulation.  With dev_lambda, differential attention: heads 2 j and 2 j + 1 of a kv-head's group are the two maps
+ * of pair j, the output is their difference sum_i (p_i - lambda p'_i) V_i (conf_kv_attend_diff).
+ * The handle gives B, Hq, Hkv, D and the softmax scale; nothing of its cache changes, and the lengths are the caller's, on the
+ * device: a recorded call moves on with them.  A token's key that is infinite or NaN shows in the rows that see it
+ * and in no other.  Rows that no sequence claims are left as they were; two sequences claim no row and write to no page together
+ * (pages that both only read are shared freely).
+ * CONF_KV_ERR_INVALID_ARG beyond the limits noted above, where max_pages * page_tokens is more than max_paged (rounded up to whole
+ * pages), and for tensors that overlap what is written.  Tensors are 16-byte aligned, tokens * n_q_heads * B at most 2^30. */
+int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const conf_kv_chunk *chunk, conf_kv_stream stream);
+
+/* conf_kv_load_prefill from pages: the cache of the layer becomes the first T0 tokens of every sequence (dev_ema0 fp32
+ * [B][Hkv][T0], or NULL).  Same result, call order and errors; T0 at most max_pages * page_tokens (CONF_KV_ERR_INVALID_ARG). */
+int conf_kv_load_pages(conf_kv_handle *h, int32_t layer, const conf_kv_pages *pages, int32_t T0, const float *dev_ema0,
+                       conf_kv_stream stream);
 
 /* Importance from the prompt's own attention (the step before the decode loop: the cache's
  * initial importance comes from an observation window of queries at the end of the prompt

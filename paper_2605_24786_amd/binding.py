@@ -33,13 +33,15 @@ class ConfKVConfig(C.Structure):
         ("n_tight", C.POINTER(C.c_int32)), ("n_loose", C.POINTER(C.c_int32)),
         ("mass_gain", C.c_float), ("ranker", C.c_int32), ("rank_scope", C.c_int32),
         ("ranker_seed", C.c_uint64), ("scale_mode", C.c_int32), ("max_chunk", C.c_int32),
-        ("evict_page", C.c_int32), ("layout", C.c_int32), ("max_shared", C.c_int32),
+        ("evict_page", C.c_int32), ("layout", C.c_int32), ("max_shared", C.c_int32), ("max_paged", C.c_int32),
     ]
 
 
-# conf_kv_prefix, conf_kv_qkv and conf_kv_constraints field by field (native alignment): packed into bytes, which a call hands over
+# conf_kv_prefix, conf_kv_pages, conf_kv_chunk, conf_kv_qkv and conf_kv_constraints field by field (native alignment): packed into bytes, which a call hands over
 # faster than a ctypes.Structure with as many fields.
 _PREFIX = struct.Struct("@2PqiP")
+_PAGES = struct.Struct("@2P3q2iPqi4x")
+_CHUNK = struct.Struct("@2i8Pq")
 _QKV = struct.Struct("@2i3P6q4P4if3P")
 _CONSTRAINTS = struct.Struct("@2iPqPPq8P2i2P")
 TYPE_FP32, TYPE_FP16, TYPE_BF16 = 0, 1, 2
@@ -72,6 +74,8 @@ SYMBOLS = {
     "conf_kv_attend": (C.c_int, [_P, C.c_int32, _P, _P, _P, _P, _P]),
     "conf_kv_attend_chunk": (C.c_int, [_P, C.c_int32, C.c_int32, _P, _P, _P, _P, _P]),
     "conf_kv_attend_shared": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_char_p, _P, _P, _P, _P, _P]),
+    "conf_kv_attend_pages": (C.c_int, [_P, C.c_char_p, C.c_char_p, _P]),
+    "conf_kv_load_pages": (C.c_int, [_P, C.c_int32, C.c_char_p, C.c_int32, _P, _P]),
     "conf_kv_observe": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
     "conf_kv_observe_prompt": (C.c_int, [_P, C.c_int32, _P, _P]),
     "conf_kv_step": (C.c_int, [_P, _P, _P, _P, _P]),
@@ -141,7 +145,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, vocab, capacit
                 protected_window, n_tight: Sequence[int], n_loose: Sequence[int], tau=0.7, alpha=0.65,
                 ema_decay=0.9, sm_scale=None, w_entropy=0.4, w_margin=0.3, w_top=0.3, mass_gain=None,
                 ranker="composite", rank_scope="kv_head", ranker_seed=0, scale_mode="token", max_chunk=0,
-                evict_page=0, layout="contiguous", max_shared=0):
+                evict_page=0, layout="contiguous", max_shared=0, max_paged=0):
     """A ConfKVConfig plus the two int32 arrays it points to (keep the tuple alive)."""
     nt = (C.c_int32 * len(n_tight))(*[int(x) for x in n_tight])
     nl = (C.c_int32 * len(n_loose))(*[int(x) for x in n_loose])
@@ -152,7 +156,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, vocab, capacit
                        w_entropy, w_margin, w_top, nt, nl,
                        -1.0 if mass_gain is None else float(mass_gain), RANKERS[ranker],
                        RANK_SCOPES[rank_scope], int(ranker_seed), SCALE_MODES[scale_mode], int(max_chunk),
-                       int(evict_page), LAYOUTS[layout], int(max_shared))
+                       int(evict_page), LAYOUTS[layout], int(max_shared), int(max_paged))
     return cfg, nt, nl
 
 
@@ -275,6 +279,64 @@ class ConfKV:
         return self._check(self.lib.conf_kv_attend_shared(self.h, layer, tq, prefix, want("q16", q16, half, rows),
                                                           want("knew16", knew16, half, new), want("vnew16", vnew16, half, new),
                                                           want("out16", out16, half, rows), self._current_stream()), "conf_kv_attend_shared")
+
+    def _pages(self, pages_k, pages_v, table):
+        """conf_kv_pages of two float16 tensors [pages][page][Hkv][D] and an int32 table [B][pages per sequence]."""
+        B, H, D, half, device = self._batch, self._kv_heads, self._head_dim, self._half, self._device
+        shape, apart = pages_k.shape, pages_k.stride()
+        if (len(shape) != 4 or shape[2:] != (H, D) or pages_k.dtype is not half or pages_k.get_device() != device or
+                pages_v.shape != shape or pages_v.dtype is not half or pages_v.get_device() != device or apart[3] != 1 or
+                pages_v.stride() != apart):
+            raise ValueError(f"pages_k, pages_v: float16 [pages][page][{H}][{D}] with dense heads and equal strides on "
+                             f"{self.state.device} are wanted, got {pages_k.dtype} {tuple(shape)} {apart} and {pages_v.dtype} "
+                             f"{tuple(pages_v.shape)} {pages_v.stride()} on {pages_k.device} and {pages_v.device}")
+        rows = table.shape
+        step = table.stride()
+        if len(rows) != 2 or rows[0] != B or table.dtype is not self._i32 or table.get_device() != device or (rows[1] > 1 and step[1] != 1):
+            raise ValueError(f"table: int32 [{B}][pages per sequence] with dense rows on {self.state.device} is wanted, got {table.dtype} "
+                             f"{tuple(rows)} {step} on {table.device}")
+        return _PAGES.pack(pages_k.data_ptr(), pages_v.data_ptr(), apart[0], apart[1], apart[2], shape[1], shape[0], table.data_ptr(),
+                           step[0] if B > 1 else rows[1], rows[1])
+
+    def attend_pages(self, q16, knew16, vnew16, out16, pages_k, pages_v, table, context, tokens=None, starts=None, new=None, lam=None):
+        """New tokens of every sequence over a paged cache pages_k, pages_v float16 [pages][page][Hkv][D] (any order of the dimensions
+        in memory with dense heads) with table int32 [B][pages per sequence], in which sequence b has context[b] tokens (int32 [B]).
+        q16 [B][T][Hq][D], knew16 / vnew16 [B][T][Hkv][D] (None: the pages hold them); or rows [R][..][D] of which sequence b has
+        starts[b] .. starts[b] + new[b] - 1 (int32 [B]), at most `tokens` of them.  out16 [..][Hq][D], with
+        lam float32 [..][Hq / 2] or [Hq / 2], the weights of the second maps, [..][Hq / 2][D]."""
+        H, Hq, D, want, half, i32 = self._kv_heads, self._q_heads, self._head_dim, self._want, self._half, self._i32
+        lead = q16.shape[:-2]
+        rows = 1
+        for n in lead:
+            rows *= n
+        if len(lead) == 2:
+            tokens = lead[1] if tokens is None else tokens
+            if lead[0] != self._batch or tokens > lead[1]:
+                raise ValueError(f"q16: [{self._batch}][T][{Hq}][{D}] is wanted, got {tuple(q16.shape)} with {tokens} tokens")
+            if starts is None and tokens != lead[1]:
+                raise ValueError("tokens: fewer than the rows of a sequence need `starts`")
+        elif len(lead) != 1 or starts is None or tokens is None:
+            raise ValueError("q16: [B][T][Hq][D], or [R][Hq][D] with `starts` and `tokens`, is wanted")
+        row = (self._batch,)
+        outs, weights, apart = Hq, 0, 0
+        if lam is not None:
+            outs = Hq // 2
+            if lam.shape == (outs,):
+                weights = want("lam", lam, self._f32, (outs,))
+            else:
+                weights, apart = want("lam", lam, self._f32, (*lead, outs)), outs
+        fresh = (*lead, H, D)
+        chunk = _CHUNK.pack(tokens, rows, want("starts", starts, i32, row), want("new", new, i32, row), want("context", context, i32, row),
+                            want("q16", q16, half, (*lead, Hq, D)), want("knew16", knew16, half, fresh), want("vnew16", vnew16, half, fresh),
+                            want("out16", out16, half, (*lead, outs, D)), weights, apart)
+        return self._check(self.lib.conf_kv_attend_pages(self.h, self._pages(pages_k, pages_v, table), chunk, self._current_stream()),
+                           "conf_kv_attend_pages")
+
+    def load_pages(self, layer: int, pages_k, pages_v, table, tokens: int, ema0=None):
+        """load_prefill of the first `tokens` tokens of every sequence from pages (see attend_pages)."""
+        return self._check(self.lib.conf_kv_load_pages(
+            self.h, layer, self._pages(pages_k, pages_v, table), tokens,
+            self._want("ema0", ema0, self._f32, (self._batch, self._kv_heads, tokens)), self._current_stream()), "conf_kv_load_pages")
 
     def observe(self, layer: int, first: int, q16, out16=None):
         """q16 / out16 [B][tq][Hq][D]: queries of the cached slots first .. first + tq - 1; out16 optional."""
@@ -474,6 +536,7 @@ def from_workload(wl, **override) -> ConfKV:
               ranker=getattr(wl, "ranker", "composite"), rank_scope=getattr(wl, "rank_scope", "kv_head"),
               ranker_seed=getattr(wl, "ranker_seed", 0), scale_mode=getattr(wl, "scale_mode", "token"),
               max_chunk=getattr(wl, "max_chunk", 0), evict_page=getattr(wl, "evict_page", 0),
-              layout=getattr(wl, "layout", "contiguous"), max_shared=getattr(wl, "max_shared", 0))
+              layout=getattr(wl, "layout", "contiguous"), max_shared=getattr(wl, "max_shared", 0),
+              max_paged=getattr(wl, "max_paged", 0))
     kw.update(override)
     return ConfKV(**kw)

@@ -28,7 +28,7 @@ struct StateLayout {
 };
 
 struct ScratchLayout {
-  size_t conf_partial, part_ml, part_o, shared_ml, shared_o, spill, score, src, sel, shared, total;
+  size_t conf_partial, part_ml, part_o, shared_ml, shared_o, paged, spill, score, src, sel, shared, total;
   size_t zero_bytes;     // [0, zero_bytes) holds the counters and is zeroed at create
 };
 
@@ -59,6 +59,7 @@ bool config_ok(const conf_kv_config *c) {
   if (c->scale_mode != CONF_KV_SCALES_TOKEN && c->scale_mode != CONF_KV_SCALES_CHANNEL) return false;
   if (c->scale_mode == CONF_KV_SCALES_CHANNEL && (c->head_dim != 128 || c->fp16_window < 0)) return false;
   if (c->max_chunk < 0 || c->max_shared < 0 || c->max_shared > 1 << 30) return false;
+  if (c->max_paged < 0 || c->max_paged > 1 << 30) return false;
   // multi-token calls: one tile of 16 query rows per unit, or up to kWideRowsMax rows on the
   // many-rows kernel (per-token scales only)
   if (c->max_chunk > 1) {
@@ -144,6 +145,8 @@ ScratchLayout scratch_layout(const conf_kv_config *c) {
   const size_t parts = shared_parts_most(c->max_shared);
   s.shared_ml = take(UPL * parts * R * sizeof(float2));
   s.shared_o = take(UPL * parts * R * D * sizeof(float));
+  // those of the parts of a paged cache
+  s.paged = take(c->max_paged > kPagesLeastPart ? pages_scratch_floats((int)D) * sizeof(float) : 0);
   // the two-launch form's scores, or the prompt-phase kernels' statistics; their parts also take the two arrays behind
   // this one, which only conf_kv_evict_compact uses
   s.spill = take(std::max(attend_spill_floats((int)UPL, (int)R, c->capacity),
@@ -333,16 +336,58 @@ int conf_kv_destroy(conf_kv_handle *h) {
   return CONF_KV_OK;
 }
 
-int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16, const void *dev_v16,
-                         int32_t T0, const float *dev_ema0, conf_kv_stream stream) {
-  if (!h) return CONF_KV_ERR_INVALID_ARG;
-  if (layer < 0 || layer >= h->cfg.n_layers) return CONF_KV_ERR_BAD_LAYER;
-  if (T0 < 0) return CONF_KV_ERR_INVALID_ARG;
-  if (T0 > 0 && (!dev_k16 || !dev_v16)) return CONF_KV_ERR_INVALID_ARG;
-  if (((uintptr_t)dev_k16 | (uintptr_t)dev_v16) & 15) return CONF_KV_ERR_INVALID_ARG;   // rows are read in 16-byte pieces
+// A call launches on the current device, a handle's memory is on the one it was created on.
+static bool on_its_device(const conf_kv_handle *h) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == h->device;
+}
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+// Values from the first to the last of the pages' rows; 0 where rows overlap or a size or stride is out of bounds.
+static long long pages_extent(const conf_kv_handle *h, const conf_kv_pages &p) {
+  constexpr int64_t kMostStride = (int64_t)1 << 40;
+  struct Dim { long long size, stride; } d[3] = {{p.n_pages, p.page_stride}, {p.page_tokens, p.token_stride}, {h->cfg.n_kv_heads, p.head_stride}};
+  std::sort(d, d + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride || (x.stride == y.stride && x.size < y.size); });
+  long long extent = h->cfg.head_dim;
+  for (const Dim &x : d) {
+    if (x.stride < 0 || x.stride > kMostStride || x.stride % 8) return 0;
+    if (x.size == 1) continue;
+    if (x.stride < extent || x.size > ((long long)1 << 56) / x.stride) return 0;
+    extent += (x.size - 1) * x.stride;
+  }
+  return extent;
+}
+static bool pages_ok(const conf_kv_handle *h, const conf_kv_pages &p) {
+  if (!p.dev_k16 || !p.dev_v16 || !p.dev_table) return false;
+  if ((((uintptr_t)p.dev_k16 | (uintptr_t)p.dev_v16) & 15) || ((uintptr_t)p.dev_table & 3)) return false;
+  if (p.page_tokens < 8 || p.page_tokens > 1 << 20 || (p.page_tokens & (p.page_tokens - 1))) return false;
+  if (p.n_pages < 1 || p.n_pages > 1 << 30 || p.max_pages < 1 || (long long)p.max_pages * p.page_tokens > 1ll << 30) return false;
+  if (p.table_stride < p.max_pages || p.table_stride > (int64_t)1 << 40) return false;
+  return pages_extent(h, p) > 0;
+}
+static PagesView pages_view(const conf_kv_pages &p) {
+  PagesView v{};
+  v.k = (__half *)p.dev_k16;
+  v.v = (__half *)p.dev_v16;
+  v.page_stride = p.page_stride;
+  v.token_stride = p.token_stride;
+  v.head_stride = p.head_stride;
+  v.table = p.dev_table;
+  v.table_stride = p.table_stride;
+  v.max_pages = p.max_pages;
+  v.n_pages = p.n_pages;
+  while ((1 << v.lg) < p.page_tokens) ++v.lg;
+  return v;
+}
+
+static int load_prompt(conf_kv_handle *h, int32_t layer, const void *dev_k16, const void *dev_v16, const PagesView *pages, int32_t T0,
+                       const float *dev_ema0, conf_kv_stream stream) {
   if (T0 > h->cfg.capacity - 1) return CONF_KV_ERR_CAPACITY;
   if (h->cv.page_lg && T0 - h->cfg.fp16_window > (h->cv.npages << h->cv.page_lg)) return CONF_KV_ERR_CAPACITY;
-  CK_HIP(h, launch_load_prefill(h->cv, layer, (const __half *)dev_k16, (const __half *)dev_v16, T0,
+  CK_HIP(h, launch_load_prefill(h->cv, layer, (const __half *)dev_k16, (const __half *)dev_v16, pages, T0,
                                 dev_ema0, (hipStream_t)stream));
   h->len_ub[layer] = T0;
   h->prompt_loaded = true;
@@ -350,6 +395,70 @@ int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16, 
   const size_t UPL = (size_t)h->cfg.batch * h->cfg.n_kv_heads;
   std::fill(h->scaled.begin() + layer * UPL, h->scaled.begin() + (layer + 1) * UPL, (uint8_t)1);
   h->fresh_len[layer] = T0;
+  return CONF_KV_OK;
+}
+
+int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16, const void *dev_v16,
+                         int32_t T0, const float *dev_ema0, conf_kv_stream stream) {
+  if (!h) return CONF_KV_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= h->cfg.n_layers) return CONF_KV_ERR_BAD_LAYER;
+  if (T0 < 0) return CONF_KV_ERR_INVALID_ARG;
+  if (T0 > 0 && (!dev_k16 || !dev_v16)) return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)dev_k16 | (uintptr_t)dev_v16) & 15) return CONF_KV_ERR_INVALID_ARG;   // rows are read in 16-byte pieces
+  return load_prompt(h, layer, dev_k16, dev_v16, nullptr, T0, dev_ema0, stream);
+}
+
+int conf_kv_load_pages(conf_kv_handle *h, int32_t layer, const conf_kv_pages *pages, int32_t T0, const float *dev_ema0,
+                       conf_kv_stream stream) {
+  if (!h || !pages) return CONF_KV_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= h->cfg.n_layers) return CONF_KV_ERR_BAD_LAYER;
+  if (T0 < 0 || !pages_ok(h, *pages) || T0 > (long long)pages->max_pages * pages->page_tokens) return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)dev_ema0 & 3) || !on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
+  const PagesView view = pages_view(*pages);
+  return load_prompt(h, layer, nullptr, nullptr, &view, T0, dev_ema0, stream);
+}
+
+int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const conf_kv_chunk *chunk, conf_kv_stream stream) {
+  if (!h || !pages || !chunk || !pages_ok(h, *pages)) return CONF_KV_ERR_INVALID_ARG;
+  const conf_kv_chunk &c = *chunk;
+  const int B = h->cfg.batch, Hq = h->cfg.n_q_heads, H = h->cfg.n_kv_heads, D = h->cfg.head_dim, G = h->cv.G;
+  const long long most = h->cfg.max_paged, page = pages->page_tokens;
+  if (most < 1 || pages->max_pages * page > (most + page - 1) / page * page) return CONF_KV_ERR_INVALID_ARG;
+  if (c.tokens < 0 || c.rows < 0 || (long long)c.tokens * Hq * B > 1ll << 30) return CONF_KV_ERR_INVALID_ARG;
+  if (!c.dev_starts && (long long)B * c.tokens > c.rows) return CONF_KV_ERR_INVALID_ARG;
+  if (c.tokens == 0 || c.rows == 0) return CONF_KV_OK;
+  if (!c.dev_context || !c.dev_q16 || !c.dev_out16 || !c.dev_knew16 != !c.dev_vnew16) return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)c.dev_q16 | (uintptr_t)c.dev_knew16 | (uintptr_t)c.dev_vnew16 | (uintptr_t)c.dev_out16) & 15) return CONF_KV_ERR_INVALID_ARG;
+  if (((uintptr_t)c.dev_starts | (uintptr_t)c.dev_new | (uintptr_t)c.dev_context | (uintptr_t)c.dev_lambda) & 3) return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_lambda && (G % 2 || c.lambda_stride < 0 || c.lambda_stride > (int64_t)1 << 40)) return CONF_KV_ERR_INVALID_ARG;
+  const size_t q_bytes = (size_t)c.rows * Hq * D * 2, new_bytes = (size_t)c.rows * H * D * 2, out_bytes = c.dev_lambda ? q_bytes / 2 : q_bytes;
+  const size_t page_bytes = (size_t)pages_extent(h, *pages) * 2;
+  if (overlap(c.dev_out16, out_bytes, c.dev_q16, q_bytes)) return CONF_KV_ERR_INVALID_ARG;
+  for (const void *plane : {pages->dev_k16, pages->dev_v16}) {
+    if (overlap(c.dev_out16, out_bytes, plane, page_bytes)) return CONF_KV_ERR_INVALID_ARG;
+    for (const void *fresh : {c.dev_knew16, c.dev_vnew16})
+      if (fresh && (overlap(fresh, new_bytes, plane, page_bytes) || overlap(fresh, new_bytes, c.dev_out16, out_bytes))) return CONF_KV_ERR_INVALID_ARG;
+    if (c.dev_knew16 && overlap(c.dev_q16, q_bytes, plane, page_bytes)) return CONF_KV_ERR_INVALID_ARG;
+  }
+  if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
+  PagesLaunch a{};
+  a.pages = pages_view(*pages);
+  a.tokens = c.tokens;
+  a.rows = c.rows;
+  a.starts = c.dev_starts;
+  a.count = c.dev_new;
+  a.context = c.dev_context;
+  a.q = (const __half *)c.dev_q16;
+  a.knew = (const __half *)c.dev_knew16;
+  a.vnew = (const __half *)c.dev_vnew16;
+  a.out = (__half *)c.dev_out16;
+  a.lambda = c.dev_lambda;
+  a.lambda_stride = c.lambda_stride;
+  a.B = B;
+  a.Hkv = H;
+  a.G = G;
+  a.sm_scale = h->cfg.sm_scale;
+  CK_HIP(h, launch_pages(a, D, h->kl.paged < h->kl.spill ? (float *)(h->scratch + h->kl.paged) : nullptr, (hipStream_t)stream));
   return CONF_KV_OK;
 }
 
@@ -389,12 +498,6 @@ static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan
   // the paged layout is read by the single-launch matrix-core kernel only
   if (h->cv.page_lg && (plan->two_launch || !plan->mfma)) return CONF_KV_ERR_BAD_SHAPE;
   return CONF_KV_OK;
-}
-
-// A call launches on the current device, a handle's memory is on the one it was created on.
-static bool on_its_device(const conf_kv_handle *h) {
-  int dev = -1;
-  return hipGetDevice(&dev) == hipSuccess && dev == h->device;
 }
 
 static bool prefix_ok(const conf_kv_handle *h, int tq, const conf_kv_prefix *p) {
@@ -576,10 +679,6 @@ int conf_kv_step_static(conf_kv_handle *h, const float *dev_logits, float *dev_c
                                       (double)h->cfg.tau, (double)h->cfg.w_entropy, (double)h->cfg.w_margin,
                                       (double)h->cfg.w_top, (hipStream_t)stream));
   return CONF_KV_OK;
-}
-
-static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
 static size_t value_bytes(int type) { return type == CONF_KV_TYPE_FP32 ? 4 : 2; }

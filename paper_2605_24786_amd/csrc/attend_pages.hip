@@ -1,0 +1,699 @@
+// Attention of a chunk of new tokens over a paged FP16 cache of the caller's (conf_kv_attend_pages).
+//
+// Rows of a kv-head are (token, head of the group), token first, so that all heads of the group share the tiles.  A workgroup takes
+// a block of rows of one (sequence, kv-head) against the keys those rows see, or against a part of them where there are fewer
+// blocks than compute units; parts leave float32 partial results which a second launch merges:
+//   ml[slot][row] = (m, l),  o[slot][row][D] = sum over the part's keys of 2^(s - m) v,   s: scores times log2(e)
+// Products are formed transposed, scores [32 keys x 32 rows] and output [D x 32 rows] (v_mfma_f32_32x32x16_f16): a lane then holds
+// values of one row only, its probabilities are the operand of the second product as they stand, and the row's statistics
+// need one exchange between two lanes.
+// The call's own keys and values are read from its arguments, never from the pages, so their way into the pages needs no wait.
+#include <algorithm>
+
+#include "confkv_dev.h"
+#include "launch.h"
+
+namespace confkv {
+
+typedef _Float16 pg_h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 pg_h4 __attribute__((ext_vector_type(4)));
+typedef short pg_s4 __attribute__((ext_vector_type(4)));
+typedef float pg_f16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPgKeys = 32;                            // keys of a wavefront's tile
+constexpr int kPgRows = 32;                            // rows of a matrix instruction's tile
+constexpr int kNoSplit = 0x7fffffff;
+
+// Per group of sixteen lanes: lane l reads four halfs of row l / 4, columns 4 (l & 3) + [0, 4), and gets half l of each row.
+__device__ __forceinline__ pg_h4 pg_read_tr(const uint8_t *p) {
+  return __builtin_bit_cast(pg_h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pg_s4 *)p));
+}
+__device__ __forceinline__ float pg_other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// The signs of the result: which of two halfs are infinite or NaN (their magnitude, 0x7c00 or more, carries into the sign).
+__device__ __forceinline__ unsigned pg_odd_halfs(int d) { return ((unsigned)d & 0x7fff7fffu) + 0x04000400u; }
+__device__ __forceinline__ unsigned pg_odd_piece(const int4 &v) {
+  return (pg_odd_halfs(v.x) | pg_odd_halfs(v.y) | pg_odd_halfs(v.z) | pg_odd_halfs(v.w)) & 0x80008000u;
+}
+__device__ __forceinline__ void pg_drop_odd(int4 &v) {
+  int *d = &v.x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) d[k] &= (int)~(((pg_odd_halfs(d[k]) & 0x80008000u) >> 15) * 0xffffu);
+}
+// LDS operations of a wavefront execute in order: between lanes that exchange data only the compiler has to keep it.
+__device__ __forceinline__ void pg_wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---------------------------------------------------------------------------------------
+// Which sequence, block of rows and part a workgroup has.  The lengths live on the device, so every workgroup works it out for
+// itself: a lane per sequence, a scan over the wavefront.
+// ---------------------------------------------------------------------------------------
+struct PgSequence {
+  int n, c, s;                                         // new tokens, tokens before them, first row of the call's tensors
+};
+__device__ __forceinline__ PgSequence pg_sequence(const PagesLaunch &a, int b) {
+  PgSequence q;
+  const int room = (int)min((long long)a.pages.max_pages << a.pages.lg, 1ll << 30);
+  q.c = min(max(a.context[b], 0), room);
+  q.n = a.count ? min(max(a.count[b], 0), a.tokens) : a.tokens;
+  q.n = min(q.n, room - q.c);
+  const int s = a.starts ? a.starts[b] : b * a.tokens;
+  q.s = min(max(s, 0), a.rows);
+  q.n = s == q.s ? min(q.n, a.rows - q.s) : 0;
+  return q;
+}
+
+struct PgJob {
+  int b, g, block, part, parts, part_keys, blocks;
+  PgSequence q;
+};
+// Parts of equal length for all sequences, the shortest for which every (block, part) has a slot; the blocks of a
+// sequence from the last one on, whose rows see the most keys.  False: the workgroup has nothing to do.
+__device__ __forceinline__ bool pg_job(const PagesLaunch &a, int rows_per_block, int quantum, unsigned x, PgJob &j) {
+  const int lane = threadIdx.x & 63;
+  j.g = x % (unsigned)a.Hkv;
+  int at = x / (unsigned)a.Hkv;
+  auto blocks_of = [&](int b, PgSequence &q) {
+    q = PgSequence{0, 0, 0};
+    if (b < a.B) q = pg_sequence(a, b);
+    return (int)(((long long)q.n * a.G + rows_per_block - 1) / rows_per_block);
+  };
+  int keys = kNoSplit;
+  PgSequence q;
+  if (a.slots > 0) {
+    long long blocks = 0, work = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+      const int mine = blocks_of(b0 + lane, q);
+      blocks += wave_sum(mine);
+      // (in quanta, so that sixty-four of them fit: at most 2^30 / 128 keys times the blocks of a call that may split)
+      const float w = (float)mine * (float)((q.c + q.n + quantum - 1) / quantum);
+      work += (long long)wave_sum(w);
+    }
+    if (blocks * a.Hkv <= a.slots && blocks > 0) {
+      long long k = max(1ll, (work * a.Hkv + a.slots - 1) / a.slots);      // quanta per part
+      for (;;) {
+        long long jobs = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+          const int mine = blocks_of(b0 + lane, q);
+          const long long len = (q.c + q.n + quantum - 1) / quantum;
+          jobs += wave_sum((int)min((long long)mine * ((len + k - 1) / k), 1ll << 20));
+        }
+        if (jobs * a.Hkv <= a.slots) break;
+        k += (k + 7) / 8;
+      }
+      keys = (int)min(k * quantum, (long long)kNoSplit);
+    }
+  }
+  j.part_keys = keys;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    const int mine = blocks_of(b0 + lane, q);
+    const int parts = keys == kNoSplit ? 1 : max(1, (q.c + q.n + keys - 1) / keys);
+    const int jobs = mine * parts, end = wave_scan_incl(jobs);
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(at < end);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      at -= __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(jobs, l);
+      j.b = b0 + l;
+      j.parts = __builtin_amdgcn_readlane(parts, l);
+      j.blocks = __builtin_amdgcn_readlane(mine, l);
+      j.block = j.blocks - 1 - at / j.parts;
+      j.part = at - (at / j.parts) * j.parts;
+      j.q.n = __builtin_amdgcn_readlane(q.n, l);
+      j.q.c = __builtin_amdgcn_readlane(q.c, l);
+      j.q.s = __builtin_amdgcn_readlane(q.s, l);
+      return true;
+    }
+    at -= __builtin_amdgcn_readlane(end, 63);
+  }
+  return false;
+}
+
+// ---------------------------------------------------------------------------------------
+// Rows of K and V of one kv-head, wherever they are.
+// ---------------------------------------------------------------------------------------
+template <int D>
+struct PgSource {
+  static constexpr int PR = D / 8, RWI = kWave / PR;   // 16-byte pieces of a row; rows that a wavefront's load covers
+  const __half *k, *v, *knew, *vnew;                   // of the kv-head
+  const int32_t *table;                                // of the sequence
+  long long page_stride, token_stride, new_stride, lane_off;
+  int lg, max_pages, n_pages, c, n;                    // tokens in front (0x7fffffff: all come from the pages), tokens in all
+
+  __device__ __forceinline__ void init(const PagesLaunch &a, const PgJob &j) {
+    const int lane = threadIdx.x & 63;
+    k = a.pages.k + j.g * a.pages.head_stride;
+    v = a.pages.v + j.g * a.pages.head_stride;
+    new_stride = (long long)a.Hkv * D;
+    knew = a.knew ? a.knew + (j.q.s * (long long)a.Hkv + j.g) * D : nullptr;
+    vnew = a.knew ? a.vnew + (j.q.s * (long long)a.Hkv + j.g) * D : nullptr;
+    table = a.pages.table + j.b * a.pages.table_stride;
+    page_stride = a.pages.page_stride;
+    token_stride = a.pages.token_stride;
+    lane_off = (lane / PR) * token_stride + (lane % PR) * 8;
+    lg = a.pages.lg;
+    max_pages = a.pages.max_pages;
+    n_pages = a.pages.n_pages;
+    c = a.knew ? j.q.c : 0x7fffffff;
+    n = j.q.c + j.q.n;
+  }
+  // the table's entry for a token (a place behind the table: its last entry; nothing read from there counts)
+  __device__ __forceinline__ int entry(int token) const { return table[min(token >> lg, max_pages - 1)]; }
+  // Offset of the lane's piece of the RWI rows from token r0 on (a multiple of RWI; so they lie in one page, whose entry is e).
+  __device__ __forceinline__ long long offset(int r0, int e) const {
+    e = min(max(e, 0), n_pages - 1);
+    return e * page_stride + (r0 & ((1 << lg) - 1)) * token_stride + lane_off;
+  }
+  __device__ __forceinline__ void load(int r0, int e, int4 &kr, int4 &vr) const {
+    const long long o = offset(r0, e);
+    const __half *kp = k + o, *vp = v + o;
+    if (r0 + RWI > c) {                                // (tokens of the call among them; behind the last one its row again)
+      const int lane = threadIdx.x & 63, t = min(r0 + lane / PR, n - 1);
+      if (t >= c) {
+        const long long m = (t - c) * new_stride + (lane % PR) * 8;
+        kp = knew + m;
+        vp = vnew + m;
+      }
+    }
+    kr = *(const int4 *)kp;
+    vr = *(const int4 *)vp;
+  }
+  __device__ __forceinline__ const __half *value_row(int t) const {
+    if (t >= c) return vnew + (t - c) * new_stride;
+    const int e = min(max(entry(t), 0), n_pages - 1);
+    return v + e * page_stride + (t & ((1 << lg) - 1)) * token_stride;
+  }
+};
+
+// ---------------------------------------------------------------------------------------
+// Thirty-two rows of a wavefront: queries, running reference, sum and output, and how many keys they see.
+// ---------------------------------------------------------------------------------------
+template <int D>
+struct PgRows {
+  pg_h8 qf[D / 16];
+  pg_f16 O[D / 32];
+  // Probabilities are 2^(score * c + off): off follows the row's maximum, and lifts it to 2^10, so that as fp16 operands they keep
+  // eleven bits down to 2^-24 of the largest (unlifted 2^-14).  One fused operation per score, whose product is not rounded;
+  // what off is rounded to is off for all keys alike.
+  float off, l;
+  int row, lim, least, most;                           // row of the block; keys the lane's row sees; the fewest and the most
+
+  static constexpr float kLift = 10.f, kSlack = 5.5f;  // 2^15.5 is 46341 of fp16's 65504
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[nt][i] = 0.f;
+    off = INFINITY;
+    l = 0.f;
+  }
+  // rows first .. first + 31 of the sequence's n * G
+  __device__ __forceinline__ void init(const PagesLaunch &a, const PgJob &j, int first) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, all = j.q.n * a.G;
+    row = first + (lane & 31);
+    const bool real = row < all;
+    const int r = min(row, all - 1), t = r / a.G, hq = r - t * a.G;
+    const __half *q = a.q + ((long long)(j.q.s + t) * a.Hkv * a.G + j.g * a.G + hq) * D;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) qf[s] = __builtin_bit_cast(pg_h8, *(const int4 *)(q + 16 * s + 8 * h));
+    lim = j.q.c + t + 1;
+    least = __builtin_amdgcn_readfirstlane(lim);       // (rows in order: the first sees least)
+    most = first < all ? __builtin_amdgcn_readlane(lim, 31) : 0;
+    row = real ? row : -1;
+    reset();
+  }
+  template <int KROW>
+  __device__ __forceinline__ void scores(const uint8_t *Kt, pg_f16 &sc) const {
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const pg_h8 kf = *(const pg_h8 *)(Kt + l32 * KROW + 32 * s + 16 * h);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[s], sc, 0, 0, 0);
+    }
+  }
+  // scores of keys key0 .. key0 + 31 -> probabilities; element i: key key0 + 8 (i / 4) + 4 h + i % 4
+  __device__ __forceinline__ void weigh(pg_f16 &sc, int key0, float c, pg_h8 (&pb)[2]) {
+    const int h = (threadIdx.x & 63) >> 5;
+    const float NEG = -INFINITY;
+    if (key0 + kPgKeys > least) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + (i & 3) < lim - key0 - 4 * h ? sc[i] : NEG;
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+    // The reference only has to stay near the maximum (the merges are exact for any), so the exchange and the rescaling run
+    // where a score passes it by more than kSlack.
+    if (__builtin_amdgcn_ballot_w64(fmaf(mx, c, off) > kLift + kSlack)) {
+      const float top = fmaxf(mx, pg_other_half(mx)) * c;
+      const float now = fminf(off, kLift - top);       // (no score yet: top is -inf and off stays)
+      const float corr = off == now ? 1.f : __builtin_amdgcn_exp2f(now - off);
+      off = now;
+      l *= corr;
+#pragma unroll
+      for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
+    }
+    const float at = off == INFINITY ? 0.f : off;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c, at));
+      l += p;
+      // (fp16 operands: half a step, 2^-11 of each probability)
+      pb[i / 8][i & 7] = (_Float16)p;
+    }
+  }
+  template <int VROW>
+  __device__ __forceinline__ void add(const uint8_t *Vt, const pg_h8 (&pb)[2]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, t16 = lane & 15, c2 = (lane >> 4) & 1;
+    const uint8_t *vp = Vt + (4 * h + (t16 >> 2)) * VROW + 32 * c2 + 8 * (t16 & 3);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int nt = 0; nt < D / 32; ++nt) {
+        const pg_h4 v0 = pg_read_tr(vp + 16 * s * VROW + 64 * nt), v1 = pg_read_tr(vp + (16 * s + 8) * VROW + 64 * nt);
+        O[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pb[s], O[nt], 0, 0, 0);
+      }
+    }
+  }
+  // Whether some channel is no number although the row's sum, of both halves, is one.
+  __device__ __forceinline__ bool odd(float sum) const {
+    float z[8] = {};
+#pragma unroll
+    for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i & 7] = fmaf(O[nt][i], 0.f, z[i & 7]);
+    const float all = ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
+    return all != all && sum == sum;
+  }
+  // The row's sum over both halves, with what the tiles left out put right.
+  __device__ __forceinline__ float finish(const PgSource<D> &src, int lo, int hi, bool dropped) {
+    const float sum = l + pg_other_half(l);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(dropped || odd(sum)) != 0ull, 0)) show_odd_values(src, lo, hi);
+    return sum;
+  }
+  // Its maximum for the merges.  (No key: -inf.  A sum that is NaN, from a score that is none, outweighs the others: a merge shall not
+  // lose it.)
+  __device__ __forceinline__ float maximum(float sum) const { return sum == sum ? -off : INFINITY; }
+  template <int OROW>
+  __device__ __forceinline__ void store_partial(float *to) const {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(float4 *)(to + 32 * nt + 8 * i + 4 * h) = make_float4(O[nt][4 * i], O[nt][4 * i + 1], O[nt][4 * i + 2], O[nt][4 * i + 3]);
+  }
+  // Values that are infinite or NaN, of the keys [lo, hi) that the lane's row sees: each makes its channel what they add up to, since a
+  // probability is positive however far the products above rounded it (where to zero, they made NaN of an infinite value, and
+  // where the values left the tile they were never met).  The first pass empties these channels, the second adds.
+  __device__ __forceinline__ void show_odd_values(const PgSource<D> &src, int lo, int hi) {
+    constexpr int PR = D / 8, RWI = kWave / PR;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    hi = min(hi, most);
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+      for (int r0 = lo; r0 < hi; r0 += RWI) {
+        const int t = min(r0 + lane / PR, hi - 1);
+        const int4 v = *(const int4 *)(src.value_row(t) + lane % PR * 8);
+        if (__builtin_amdgcn_ballot_w64(pg_odd_piece(v) != 0u) == 0ull) continue;
+#pragma unroll 1
+        for (int key = r0; key < min(r0 + RWI, hi); ++key) {
+          const __half *vr = src.value_row(key);
+#pragma unroll
+          for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const pg_h4 x4 = *(const pg_h4 *)(vr + 32 * nt + 8 * k + 4 * h);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float x = (float)x4[e];
+                const int i = 4 * k + e;
+                if (key < lim && !(fabsf(x) < INFINITY)) O[nt][i] = pass ? O[nt][i] + x : 0.f;
+              }
+            }
+        }
+      }
+    }
+  }
+};
+
+// The weight of the second map of pair row / 2 where heads are subtracted (a row is a first map's where it is even).
+__device__ __forceinline__ float pg_lambda(const PagesLaunch &a, const PgJob &j, int row) {
+  const int t = row / a.G, pair = (row - t * a.G) >> 1;
+  return a.lambda[(j.q.s + t) * a.lambda_stride + j.g * (a.G >> 1) + pair];
+}
+// Where row `row` of the sequence goes: [rows][heads][D], half of the heads where they are subtracted in pairs.
+template <int D>
+__device__ __forceinline__ __half *pg_out_row(const PagesLaunch &a, const PgJob &j, int row) {
+  const int t = row / a.G, hq = row - t * a.G, G = a.lambda ? a.G >> 1 : a.G;
+  return a.out + (((long long)(j.q.s + t) * a.Hkv + j.g) * G + (a.lambda ? hq >> 1 : hq)) * D;
+}
+
+// Weight of a partial result with maximum m beside one of maximum M.
+__device__ __forceinline__ float pg_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m - M), kLeastWeight);
+}
+// y += f x (f zero, of a result without keys: whatever x holds)
+__device__ __forceinline__ void pg_add4(float4 &y, float f, const float4 &x) {
+  if (f == 0.f) return;
+  y.x = fmaf(f, x.x, y.x);
+  y.y = fmaf(f, x.y, y.y);
+  y.z = fmaf(f, x.z, y.z);
+  y.w = fmaf(f, x.w, y.w);
+}
+// Channels d .. d + 3 of row `row`, sums y over its normaliser; sixteen neighbouring lanes hold a row, the next sixteen the next one.
+// Heads that are subtracted in pairs: the even row takes the odd one's from there.  (All lanes call it.)
+template <int D>
+__device__ __forceinline__ void pg_write_out(const PagesLaunch &a, const PgJob &j, int row, int d, float4 y, float inv) {
+  y.x *= inv;
+  y.y *= inv;
+  y.z *= inv;
+  y.w *= inv;
+  const bool real = row < j.q.n * a.G;
+  if (a.lambda) {
+    const float4 z = make_float4(__shfl_xor(y.x, 16, kWave), __shfl_xor(y.y, 16, kWave), __shfl_xor(y.z, 16, kWave), __shfl_xor(y.w, 16, kWave));
+    if (!real || (row & 1)) return;
+    const float f = pg_lambda(a, j, row);
+    y = make_float4(fmaf(-f, z.x, y.x), fmaf(-f, z.y, y.y), fmaf(-f, z.z, y.z), fmaf(-f, z.w, y.w));
+  }
+  if (real) *(pg_h4 *)(pg_out_row<D>(a, j, row) + d) = pg_h4{(_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
+}
+
+// The new tokens whose first row lies in rows [lo, hi) of the sequence go to their pages (an entry that is no page: nowhere).
+template <int D>
+__device__ __forceinline__ void pg_append(const PagesLaunch &a, const PgJob &j, int lo, int hi, int threads) {
+  if (!a.knew || j.part != 0) return;
+  constexpr int PR = D / 8;
+  const int t0 = (lo + a.G - 1) / a.G, t1 = min(j.q.n, (hi + a.G - 1) / a.G);
+  for (int i = threadIdx.x; i < (t1 - t0) * PR; i += threads) {
+    const int t = t0 + i / PR, at = j.q.c + t;
+    const int e = a.pages.table[j.b * a.pages.table_stride + (at >> a.pages.lg)];
+    if ((unsigned)e >= (unsigned)a.pages.n_pages) continue;
+    const long long from = ((j.q.s + t) * (long long)a.Hkv + j.g) * D + i % PR * 8;
+    const long long to = a.pages.offset(e, at, j.g) + i % PR * 8;
+    *(int4 *)(a.pages.k + to) = *(const int4 *)(a.knew + from);
+    *(int4 *)(a.pages.v + to) = *(const int4 *)(a.vnew + from);
+  }
+}
+
+// Tiles in LDS, rows of these strides (bytes): 16-byte pieces of eight K rows on different banks, 64-byte pieces of four V rows
+// likewise.
+template <int D>
+struct PgTile {
+  static constexpr int KROW = 2 * D + 16, VROW = 2 * D + 64;
+  static constexpr int kBytes = kPgKeys * (KROW + VROW);
+  static constexpr int OROW = D + 4;                   // floats of a partial's row where wavefronts merge
+};
+
+// ---------------------------------------------------------------------------------------
+// Up to 32 rows of a (sequence, kv-head), single tokens above all: bound by the bytes of K and V.  Eight wavefronts take the
+// part's tiles of 32 keys in turn; a wavefront waits for nobody before the merge: it loads and multiplies tiles of its own, the
+// next one in flight in registers while this one is used.
+// ---------------------------------------------------------------------------------------
+constexpr int kManyQuantum = kPagesLeastPart;
+constexpr int kFewWaves = 8, kFewQuantum = kFewWaves * kPgKeys;
+
+template <int D>
+__global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void pages_few_kernel(PagesLaunch a) {
+  using L = PgTile<D>;
+  constexpr int PR = D / 8, RWI = kWave / PR, NP = kPgKeys / RWI;
+  __shared__ __align__(16) uint8_t s_tile[kFewWaves * L::kBytes];
+  __shared__ float s_m[kFewWaves][kPgRows], s_l[kFewWaves][kPgRows];
+  static_assert(kPgRows * L::OROW * 4 <= L::kBytes, "a wavefront's partial fits its tile");
+  PgJob j;
+  if (!pg_job(a, kPgRows, kFewQuantum, blockIdx.x, j)) return;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, h = lane >> 5;
+  PgSource<D> src;
+  src.init(a, j);
+  const int first_row = j.block * kPgRows;
+  const int lo = j.part_keys == kNoSplit ? 0 : j.part * j.part_keys;
+  const int hi = (int)min((long long)lo + j.part_keys, (long long)(j.q.c + j.q.n));
+  PgRows<D> st;
+  struct Turn { int4 k[NP], v[NP]; } x;
+  auto load = [&](int base, int ent) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) src.load(base + RWI * i, __builtin_amdgcn_readlane(ent, RWI * i), x.k[i], x.v[i]);
+  };
+  int key0 = lo + w * kPgKeys;
+  int ent = 0;
+  if (key0 < hi) {
+    ent = src.entry(key0 + l32);
+    load(key0, ent);
+    ent = src.entry(key0 + kFewQuantum + l32);
+  }
+  st.init(a, j, first_row);
+  const int end = min(hi, st.most);
+  const float c = a.sm_scale * 1.44269504088896341f;
+  uint8_t *Kt = s_tile + w * L::kBytes, *Vt = Kt + kPgKeys * L::KROW;
+  bool dropped = false;
+  for (; key0 < end; key0 += kFewQuantum) {
+    // Keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN value: where there
+    // are such rows these values leave the tile here and reach the rows that do see them at the end.
+    if (key0 + kPgKeys > st.least) {
+      unsigned odd = 0u;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) odd |= pg_odd_piece(x.v[i]);
+      if (__builtin_expect(odd != 0u, 0)) {
+        dropped = true;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) pg_drop_odd(x.v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int row = RWI * i + lane / PR;
+      *(int4 *)(Kt + row * L::KROW + lane % PR * 16) = x.k[i];
+      *(int4 *)(Vt + row * L::VROW + lane % PR * 16) = x.v[i];
+    }
+    pg_wave_sync();
+    if (key0 + kFewQuantum < end) {
+      load(key0 + kFewQuantum, ent);
+      ent = src.entry(key0 + 2 * kFewQuantum + l32);
+    }
+    pg_f16 sc;
+    pg_h8 pb[2];
+    st.template scores<L::KROW>(Kt, sc);
+    st.weigh(sc, key0, c, pb);
+    st.template add<L::VROW>(Vt, pb);
+    pg_wave_sync();
+  }
+  const float sum = st.finish(src, lo, hi, dropped);
+  // (no key: -inf stays; a sum that is NaN, from a score that is none, outweighs the others: a merge shall not lose it)
+  if (h == 0) {
+    s_m[w][l32] = st.maximum(sum);
+    s_l[w][l32] = sum;
+  }
+  st.template store_partial<L::OROW>((float *)(s_tile + w * L::kBytes) + l32 * L::OROW);
+  pg_append<D>(a, j, first_row, first_row + kPgRows, kFewWaves * kWave);
+  __syncthreads();
+  // sixteen threads per row merge the wavefronts' partials
+  const int row = tid >> 4;
+  float m[kFewWaves], M = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int k = 0; k < kFewWaves; ++k) {
+    m[k] = s_m[k][row];
+    M = fmaxf(M, m[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kFewWaves; ++k) {
+    m[k] = pg_weight(m[k], M);
+    l = m[k] == 0.f ? l : fmaf(m[k], s_l[k][row], l);
+  }
+#pragma unroll
+  for (int p = 0; p < D / 64; ++p) {
+    const int d = (tid & 15) * 4 + 64 * p;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
+    if (j.parts == 1) {
+      pg_write_out<D>(a, j, first_row + row, d, y, 1.f / l);
+    } else {
+      *(float4 *)(a.o + ((long long)blockIdx.x * kPgRows + row) * D + d) = y;
+    }
+  }
+  if (j.parts > 1 && (tid & 15) == 0) a.ml[(long long)blockIdx.x * kPgRows + row] = make_float2(M, l);
+}
+
+// ---------------------------------------------------------------------------------------
+// More rows: bound by the matrix products and the exponentials.  Four wavefronts of 32 * RB rows each share tiles of 64 keys in LDS,
+// two buffers, one barrier per tile; the tile after the next is in flight in registers.
+// ---------------------------------------------------------------------------------------
+constexpr int kManyWaves = 4, kManyKeys = 64, kManyThreads = kManyWaves * kWave;
+
+template <int D, int RB>
+__global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB == 1 ? 2 : 1, RB == 1 ? 2 : 1))) void pages_many_kernel(PagesLaunch a) {
+  using L = PgTile<D>;
+  constexpr int PR = D / 8, RWI = kWave / PR, RPP = kManyThreads / PR, NP = kManyKeys / RPP, R = kManyWaves * RB * kPgRows;
+  constexpr int kKBytes = kManyKeys * L::KROW, kBuffer = 2 * L::kBytes;
+  __shared__ __align__(16) uint8_t s_tile[2 * kBuffer];
+  __shared__ int s_bad[2];
+  PgJob j;
+  if (!pg_job(a, R, kManyQuantum, blockIdx.x, j)) return;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  PgSource<D> src;
+  src.init(a, j);
+  const int first_row = j.block * R, last_row = min(first_row + R, j.q.n * a.G) - 1;
+  const int lo = j.part_keys == kNoSplit ? 0 : j.part * j.part_keys;
+  const int seen = j.q.c + last_row / a.G + 1;           // keys that the block's last row sees
+  const int hi = (int)min((long long)lo + j.part_keys, (long long)seen);
+  const int all_least = j.q.c + first_row / a.G + 1;
+  struct Turn { int4 k[NP], v[NP]; } x;
+  auto load = [&](int base, int ent) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = RPP * i + RWI * w;
+      src.load(base + r, __builtin_amdgcn_readlane(ent, r), x.k[i], x.v[i]);
+    }
+  };
+  int ent = src.entry(lo + lane);
+  if (lo < hi) {
+    load(lo, ent);
+    ent = src.entry(lo + kManyKeys + lane);
+  }
+  PgRows<D> st[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) st[rb].init(a, j, first_row + (w * RB + rb) * kPgRows);
+  const float c = a.sm_scale * 1.44269504088896341f;
+  // (see pages_few_kernel)
+  auto store = [&](int turn, int base) {
+    if (base + kManyKeys > all_least) {
+      unsigned odd = 0u;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) odd |= pg_odd_piece(x.v[i]);
+      if (__builtin_expect(odd != 0u, 0)) {
+        s_bad[turn & 1] = turn;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) pg_drop_odd(x.v[i]);
+      }
+    }
+    uint8_t *Kt = s_tile + (turn & 1) * kBuffer, *Vt = Kt + kKBytes;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int row = tid / PR + RPP * i;
+      *(int4 *)(Kt + row * L::KROW + tid % PR * 16) = x.k[i];
+      *(int4 *)(Vt + row * L::VROW + tid % PR * 16) = x.v[i];
+    }
+  };
+  if (tid < 2) s_bad[tid] = -1;
+  __syncthreads();
+  bool dropped = false;
+  if (lo < hi) {
+    store(0, lo);
+    if (lo + kManyKeys < hi) {
+      load(lo + kManyKeys, ent);
+      ent = src.entry(lo + 2 * kManyKeys + lane);
+    }
+  }
+  __syncthreads();
+  int turn = 0;
+  for (int base = lo; base < hi; base += kManyKeys, ++turn) {
+    if (base + kManyKeys < hi) store(turn + 1, base + kManyKeys);
+    if (base + 2 * kManyKeys < hi) {
+      load(base + 2 * kManyKeys, ent);
+      ent = src.entry(base + 3 * kManyKeys + lane);
+    }
+    const uint8_t *Kt = s_tile + (turn & 1) * kBuffer, *Vt = Kt + kKBytes;
+    dropped |= s_bad[turn & 1] == turn;
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int key0 = base + sub * kPgKeys;
+      {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          if (key0 >= min(hi, st[rb].most)) continue;
+          pg_f16 sc;
+          pg_h8 pb[2];
+          st[rb].template scores<L::KROW>(Kt + sub * kPgKeys * L::KROW, sc);
+          st[rb].weigh(sc, key0, c, pb);
+          st[rb].template add<L::VROW>(Vt + sub * kPgKeys * L::VROW, pb);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  pg_append<D>(a, j, first_row, first_row + R, kManyThreads);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const float l = st[rb].finish(src, lo, hi, dropped);
+    // the wavefront's rows through LDS, its own share of the tiles' room, so that they leave as whole rows
+    float *wo = (float *)(s_tile + w * L::kBytes);
+    st[rb].template store_partial<L::OROW>(wo + (lane & 31) * L::OROW);
+    pg_wave_sync();
+    const float m = st[rb].maximum(l);
+#pragma unroll
+    for (int p = 0; p < kPgRows / 4; ++p) {
+      const int r = 4 * p + (lane >> 4), row = first_row + (w * RB + rb) * kPgRows + r;
+      const float lr = __shfl(l, r, kWave);
+#pragma unroll
+      for (int q = 0; q < D / 64; ++q) {
+        const int d = (lane & 15) * 4 + 64 * q;
+        const float4 y = *(const float4 *)(wo + r * L::OROW + d);
+        if (j.parts == 1) pg_write_out<D>(a, j, row, d, y, 1.f / lr);
+        else *(float4 *)(a.o + ((long long)blockIdx.x * R + (w * RB + rb) * kPgRows + r) * D + d) = y;
+      }
+    }
+    if (j.parts > 1 && lane < kPgRows) a.ml[(long long)blockIdx.x * R + (w * RB + rb) * kPgRows + lane] = make_float2(m, l);
+    pg_wave_sync();
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// The parts' partial results of a block of R rows, merged: sixteen threads per row.
+// ---------------------------------------------------------------------------------------
+template <int D, int R>
+__global__ __launch_bounds__(256) void pages_merge_kernel(PagesLaunch a, int quantum) {
+  PgJob j;
+  if (!pg_job(a, R, quantum, blockIdx.x, j) || j.parts == 1 || j.part != 0) return;
+  const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row);
+  for (int r0 = 0; r0 < rows; r0 += 16) {
+    const int r = r0 + (threadIdx.x >> 4);               // (past the last row: partials that nothing reads)
+    const float2 *ml = a.ml + (long long)blockIdx.x * R + r;
+    const float *o = a.o + ((long long)blockIdx.x * R + r) * D;
+    const long long apart = (long long)a.Hkv * R;
+    float M = -INFINITY, l = 0.f;
+    for (int p = 0; p < j.parts; ++p) M = fmaxf(M, ml[p * apart].x);
+    float4 y[D / 64];
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < j.parts; ++p) {
+      const float2 s = ml[p * apart];
+      const float f = pg_weight(s.x, M);
+      l = f == 0.f ? l : fmaf(f, s.y, l);
+#pragma unroll
+      for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f, *(const float4 *)(o + p * apart * D + (threadIdx.x & 15) * 4 + 64 * q));
+    }
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + r, (threadIdx.x & 15) * 4 + 64 * q, y[q], 1.f / l);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------
+// Rows of a block: one tile where a sequence's rows fit it, else 128.
+int pages_block_rows(int tokens, int G) { return (long long)tokens * G <= kPgRows ? kPgRows : kManyWaves * kPgRows; }
+
+size_t pages_scratch_floats(int D) { return (size_t)kPagesSlots * kManyWaves * kPgRows * (D + 2); }
+
+hipError_t launch_pages(PagesLaunch a, int D, float *scratch, hipStream_t stream) {
+  const int R = pages_block_rows(a.tokens, a.G), quantum = R == kPgRows ? kFewQuantum : kManyQuantum;
+  // blocks that there can be at most; fewer than the slots: the call may be split
+  const long long most = (long long)a.B * (((long long)a.tokens * a.G + R - 1) / R) * a.Hkv;
+  if (most > 0x7fffffffll) return hipErrorInvalidValue;
+  // Without counts of their own all sequences have `tokens` each: the blocks are known, and where they fill the slots none is cut.
+  a.slots = scratch && (a.count || most <= kPagesSlots) ? kPagesSlots : 0;
+  a.ml = (float2 *)scratch;
+  a.o = scratch + (size_t)kPagesSlots * R * 2;
+  const dim3 grid((unsigned)std::max<long long>(most, a.slots));
+#define CONFKV_CASE(d)                                                                                                          if (D == d) {                                                                                                                   if (R == kPgRows) {                                                                                                             hipLaunchKernelGGL(pages_few_kernel<d>, grid, dim3(kFewWaves * kWave), 0, stream, a);                                         if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<d, kPgRows>), dim3(a.slots), dim3(256), 0, stream, a, quantum);                      } else {                                                                                                                        hipLaunchKernelGGL((pages_many_kernel<d, 1>), grid, dim3(kManyThreads), 0, stream, a);                                        if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<d, kManyWaves * kPgRows>), dim3(a.slots), dim3(256), 0, stream, a, quantum);         }                                                                                                                           }
+  CONFKV_CASE(64) CONFKV_CASE(128)
+#undef CONFKV_CASE
+  return hipGetLastError();
+}
+
+}  // namespace confkv

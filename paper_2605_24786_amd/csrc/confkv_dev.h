@@ -84,6 +84,21 @@ __device__ __forceinline__ int slot_row(const CacheView &cv, const int32_t *tab,
   return cv.cap - cv.cap16 + r;
 }
 
+// A paged FP16 cache of the caller's (conf_kv_pages); strides in values.
+struct PagesView {
+  __half *k, *v;
+  long long page_stride, token_stride, head_stride, table_stride;
+  const int32_t *table;              // [B][max_pages], rows table_stride entries apart
+  int max_pages, n_pages, lg;        // a page holds 2^lg tokens
+  // page of a token of a sequence's table row, held within the pages there are
+  __device__ __forceinline__ int page_of(const int32_t *row, int token) const {
+    return min(max(row[min(token >> lg, max_pages - 1)], 0), n_pages - 1);
+  }
+  __device__ __forceinline__ long long offset(int page, int token, int head) const {
+    return page * page_stride + (token & ((1 << lg) - 1)) * token_stride + head * head_stride;
+  }
+};
+
 // Per layer: tokens appended by conf_kv_attend / conf_kv_attend_chunk since the last commit.
 struct LayerMask {
   unsigned char c[kMaxLayers];

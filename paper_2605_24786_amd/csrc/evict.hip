@@ -110,20 +110,24 @@ __device__ __forceinline__ void quantize_row_channels(const __half *__restrict__
 // owns the 8 channels of 16-byte piece t % 16 on the rows t / 16, t / 16 + 64, ...;
 // scale_d = fl16(fl32(max_t |x_{t,d}| / 127)), 0 when that is not finite.
 // ---------------------------------------------------------------------------------------
+// (kPages: the prompt's rows lie in pages; here and in the loader.)
+template <bool kPages>
 __global__ __launch_bounds__(1024) void channel_scales_kernel(CacheView cv, int layer,
                                                               const __half *__restrict__ k16,
-                                                              const __half *__restrict__ v16, int T0) {
+                                                              const __half *__restrict__ v16, PagesView pages, int T0) {
   constexpr int D = 128, PIECES = D / 8, ROWS = 1024 / PIECES;
   __shared__ unsigned short part[ROWS][D];
   const int ul = blockIdx.x, tid = threadIdx.x;
   const int u = layer * cv.B * cv.Hkv + ul;
   const int c = tid % PIECES, r0 = tid / PIECES;
-  const __half *src = (blockIdx.y ? v16 : k16) + (size_t)ul * T0 * D;
+  const __half *src = kPages ? (blockIdx.y ? pages.v : pages.k) : (blockIdx.y ? v16 : k16) + (size_t)ul * T0 * D;
+  const int32_t *table = kPages ? pages.table + ul / cv.Hkv * pages.table_stride : nullptr;
   // |x| as fp16 bits with the sign cleared: for finite values and infinities the bit patterns
   // order like the magnitudes, so the maximum is taken on 16-bit integers
   unsigned short m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int t = r0; t < T0; t += ROWS) {
-    const int4 raw = *(const int4 *)(src + (size_t)t * D + c * 8);
+    const long long row = kPages ? pages.offset(pages.page_of(table, t), t, ul % cv.Hkv) : (long long)t * D;
+    const int4 raw = *(const int4 *)(src + row + c * 8);
     const unsigned w[4] = {(unsigned)raw.x, (unsigned)raw.y, (unsigned)raw.z, (unsigned)raw.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -211,9 +215,9 @@ __device__ __forceinline__ uint2 quantize_piece_channels(const int4 &raw, const 
   return pack_codes8(code);
 }
 
-template <int D>
+template <int D, bool kPages>
 __global__ __launch_bounds__(kEvThreads) void load_prefill_kernel(
-    CacheView cv, int layer, const __half *__restrict__ k16, const __half *__restrict__ v16, int T0,
+    CacheView cv, int layer, const __half *__restrict__ k16, const __half *__restrict__ v16, PagesView pages, int T0,
     const float *__restrict__ ema0) {
   constexpr int LPR = D / 8, RW = kEvThreads / LPR;
   const int c = threadIdx.x % LPR;
@@ -235,8 +239,10 @@ __global__ __launch_bounds__(kEvThreads) void load_prefill_kernel(
   // traffic: streaming loads and stores, so the loader leaves the caches to the decode kernels
   typedef int v4i_t __attribute__((ext_vector_type(4)));
   typedef unsigned v2u_t __attribute__((ext_vector_type(2)));
-  const v4i_t kl = __builtin_nontemporal_load((const v4i_t *)(k16 + ((size_t)ul * T0 + t) * D + c * 8));
-  const v4i_t vl = __builtin_nontemporal_load((const v4i_t *)(v16 + ((size_t)ul * T0 + t) * D + c * 8));
+  long long from = ((long long)ul * T0 + t) * D;
+  if constexpr (kPages) from = pages.offset(pages.page_of(pages.table + ul / cv.Hkv * pages.table_stride, t), t, ul % cv.Hkv);
+  const v4i_t kl = __builtin_nontemporal_load((const v4i_t *)((kPages ? pages.k : k16) + from + c * 8));
+  const v4i_t vl = __builtin_nontemporal_load((const v4i_t *)((kPages ? pages.v : v16) + from + c * 8));
   const int4 kraw = make_int4(kl.x, kl.y, kl.z, kl.w), vraw = make_int4(vl.x, vl.y, vl.z, vl.w);
   if (c == 0) {
     // (identity table, ring heads 0: INT8 slot t sits in row t, FP16 slot t in metadata row t - n8)
@@ -1868,16 +1874,22 @@ void evict_unit_kernel(CacheView cv, LayerMask appended, double alpha, int32_t *
 // host side
 // ---------------------------------------------------------------------------------------
 
-hipError_t launch_load_prefill(const CacheView &cv, int layer, const __half *k16, const __half *v16,
-                               int T0, const float *ema0, hipStream_t stream) {
+template <bool kPages>
+static void launch_load(const CacheView &cv, int layer, const __half *k16, const __half *v16, const PagesView &pages, int T0,
+                        const float *ema0, hipStream_t stream) {
   const int rw = kEvThreads / (cv.D / 8);            // tokens per workgroup of the loader
   dim3 grid(T0 > 0 ? (T0 + rw - 1) / rw : 1, cv.B * cv.Hkv);
   if (cv.chan)      // D = 128 by construction of the handle
-    hipLaunchKernelGGL(channel_scales_kernel, dim3(cv.B * cv.Hkv, 2), dim3(1024), 0, stream, cv, layer, k16, v16, T0);
+    hipLaunchKernelGGL(channel_scales_kernel<kPages>, dim3(cv.B * cv.Hkv, 2), dim3(1024), 0, stream, cv, layer, k16, v16, pages, T0);
   if (cv.D == 64)
-    hipLaunchKernelGGL(load_prefill_kernel<64>, grid, dim3(kEvThreads), 0, stream, cv, layer, k16, v16, T0, ema0);
+    hipLaunchKernelGGL((load_prefill_kernel<64, kPages>), grid, dim3(kEvThreads), 0, stream, cv, layer, k16, v16, pages, T0, ema0);
   else
-    hipLaunchKernelGGL(load_prefill_kernel<128>, grid, dim3(kEvThreads), 0, stream, cv, layer, k16, v16, T0, ema0);
+    hipLaunchKernelGGL((load_prefill_kernel<128, kPages>), grid, dim3(kEvThreads), 0, stream, cv, layer, k16, v16, pages, T0, ema0);
+}
+hipError_t launch_load_prefill(const CacheView &cv, int layer, const __half *k16, const __half *v16, const PagesView *pages,
+                               int T0, const float *ema0, hipStream_t stream) {
+  if (pages) launch_load<true>(cv, layer, k16, v16, *pages, T0, ema0, stream);
+  else launch_load<false>(cv, layer, k16, v16, PagesView{}, T0, ema0, stream);
   return hipGetLastError();
 }
 

@@ -151,6 +151,25 @@ size_t shared_parts_most(int tokens);      // parts a prefix of up to that many 
 void shared_plan(int rows, int Hkv, int D, int T, int cus, int forced_row_waves, SharedPlan *plan);
 int device_cu_count();
 hipError_t launch_shared_prefix(const SharedLaunch &a, const SharedPlan &p, int D, hipStream_t stream);
+// ---- attend_pages.hip ----
+constexpr int kPagesSlots = 256;           // (block, part) pairs of a split call at most: one workgroup per compute unit
+constexpr int kPagesLeastPart = 128;       // keys that a part has at least: calls on shorter caches are not split
+struct PagesLaunch {
+  PagesView pages;
+  int tokens, rows;                        // most new tokens of a sequence, rows of the call's tensors
+  const int32_t *starts, *count, *context; // [B]; starts null: b * tokens, count null: tokens
+  const __half *q, *knew, *vnew;           // [rows][Hkv * G][D], [rows][Hkv][D] (null: the pages hold them)
+  __half *out;                             // [rows][Hkv * G or half of it][D]
+  const float *lambda;                     // null, or weights [rows][Hkv * G / 2], rows lambda_stride apart
+  long long lambda_stride;
+  int B, Hkv, G;
+  float sm_scale;
+  int slots;                               // filled in by the launcher, as ml and o
+  float2 *ml;
+  float *o;
+};
+size_t pages_scratch_floats(int D);
+hipError_t launch_pages(PagesLaunch a, int D, float *scratch, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,
 // contiguous layout).  scratch: scratch_floats floats, at least observe_scratch_floats(B * Hkv, G, T); with more the
 // work is cut into parts, observe_plan_floats(B * Hkv, G, T, first block of rows, INT8 slots, chan, scratch_floats, CUs) of them are used.
@@ -167,7 +186,8 @@ hipError_t launch_observe_prompt(const CacheView &cv, int layer, const __half *q
 // left, [6] INT8 ring head after the compaction, [7] 1 = the entries above are final for this
 // call (0 after the first ranking kernel: the unit waits for the general one).
 constexpr int kSelInts = 8;
-hipError_t launch_load_prefill(const CacheView &cv, int layer, const __half *k16, const __half *v16,
+// pages: null, or where the prompt is instead of k16 and v16
+hipError_t launch_load_prefill(const CacheView &cv, int layer, const __half *k16, const __half *v16, const PagesView *pages,
                                int T0, const float *ema0, hipStream_t stream);
 // Ranker variants; all zero = the composite ranker per (layer, kv-head).
 struct RankOptions {
