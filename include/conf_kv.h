@@ -249,7 +249,7 @@ int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16,
  *      (so sum_i A_i = G), then ema_i <- lambda * ema_i + (1 - lambda) * A_i.
  * dev_q16: fp16 [B][Hq][D]; dev_knew16 / dev_vnew16: fp16 [B][Hkv][D]; dev_out16: fp16
  * [B][Hq][D], written.  All 16-byte aligned.
- * Exactly one conf_kv_attend (conf_kv_attend_chunk, conf_kv_attend_shared) per layer between two conf_kv_evict_compact calls
+ * Exactly one conf_kv_attend (conf_kv_attend_chunk, conf_kv_attend_shared, conf_kv_attend_diff) per layer between two conf_kv_evict_compact calls
  * (CONF_KV_ERR_BAD_STATE otherwise); CONF_KV_ERR_CAPACITY, before anything is launched,
  * if the unit could already hold `capacity` tokens.
  * The workgroups that share a unit exchange partial results inside the launch, so the launch
@@ -257,7 +257,7 @@ int conf_kv_load_prefill(conf_kv_handle *h, int32_t layer, const void *dev_k16,
  * running at the same time, only delay it (its waits are bounded at several hundred
  * milliseconds); a wait that does expire leaves the call's outputs undefined and is reported by
  * conf_kv_counters (device_errors, CONF_KV_ERR_DEVICE).  Two launches of this kind on two streams
- * (other handles: conf_kv_attend, conf_kv_attend_chunk, conf_kv_attend_shared, conf_kv_observe, conf_kv_step) may each
+ * (other handles: conf_kv_attend, conf_kv_attend_chunk, conf_kv_attend_shared, conf_kv_attend_diff, conf_kv_observe, conf_kv_step) may each
  * hold compute units that the other's workgroups wait for if together they need more than the
  * device has; order such calls by events where their grids are large.  A call of this function
  * takes up to one workgroup per compute unit.  Calls of more than 16 / G tokens
@@ -307,6 +307,19 @@ typedef struct conf_kv_prefix {
  * start can be handed to conf_kv_load_prefill instead).  A recorded call keeps the prefix's place and length and reads dev_seen anew. */
 int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const conf_kv_prefix *prefix, const void *dev_q16,
                           const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream);
+
+/* conf_kv_attend_chunk with differential attention: heads 2 j and 2 j + 1 of a kv-head's group are the two maps of pair j, over the
+ * pair's keys and values, and the output is their difference,
+ *     out[b][t][j] = sum_i w_i V_i,   w_i = p_i - lambda[b][t][j] p'_i,
+ * one rounding at its end; importance is the size of the weight that a slot's value had, A_i = sum_j |w_i| (of one query; queries
+ * of a call as in conf_kv_attend_chunk).  Tensors, errors and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend) but for dev_out16,
+ * fp16 [B][tq][Hq / 2][D], and dev_lambda, fp32 [B][tq][Hq / 2] with sequences batch_stride and tokens token_stride values apart
+ * (0: the same weights for all).  An odd group or tq * n_q_heads / n_kv_heads above 16 is CONF_KV_ERR_INVALID_ARG.
+ * The norm of the outputs' heads that such models put behind it is conf_kv_prepare_qkv's (dev_q alone, rotated = 0).
+ * conf_kv_observe* see single maps: the importance they give sums to G per query, more than a step's here. */
+int conf_kv_attend_diff(conf_kv_handle *h, int32_t layer, int32_t tq, const float *dev_lambda, int64_t batch_stride,
+                        int64_t token_stride, const void *dev_q16, const void *dev_knew16, const void *dev_vnew16, void *dev_out16,
+                        conf_kv_stream stream);
 
 /* A paged FP16 cache of the caller's, in which prompts are kept while they are worked off: the rows of token t of sequence b
  * lie in page table[b][t / page_tokens], slot t % page_tokens, kv-head g's at page * page_stride + slot * token_stride +

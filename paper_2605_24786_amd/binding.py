@@ -74,6 +74,7 @@ SYMBOLS = {
     "conf_kv_attend": (C.c_int, [_P, C.c_int32, _P, _P, _P, _P, _P]),
     "conf_kv_attend_chunk": (C.c_int, [_P, C.c_int32, C.c_int32, _P, _P, _P, _P, _P]),
     "conf_kv_attend_shared": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_char_p, _P, _P, _P, _P, _P]),
+    "conf_kv_attend_diff": (C.c_int, [_P, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64, _P, _P, _P, _P, _P]),
     "conf_kv_attend_pages": (C.c_int, [_P, C.c_char_p, C.c_char_p, _P]),
     "conf_kv_load_pages": (C.c_int, [_P, C.c_int32, C.c_char_p, C.c_int32, _P, _P]),
     "conf_kv_observe": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
@@ -279,6 +280,23 @@ class ConfKV:
         return self._check(self.lib.conf_kv_attend_shared(self.h, layer, tq, prefix, want("q16", q16, half, rows),
                                                           want("knew16", knew16, half, new), want("vnew16", vnew16, half, new),
                                                           want("out16", out16, half, rows), self._current_stream()), "conf_kv_attend_shared")
+
+    def attend_diff(self, layer: int, q16, knew16, vnew16, out16, lam):
+        """q16 [B][tq][Hq][D], knew16 / vnew16 [B][tq][Hkv][D] as attend_chunk takes them, out16 [B][tq][Hq / 2][D]: the difference of
+        heads 2 j and 2 j + 1, the second times lam float32 [Hq / 2] or [B][tq][Hq / 2] (dense pairs, other strides as they are)."""
+        B, H, Hq, D, half, want = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._half, self._want
+        tq = q16.shape[1]
+        pairs = Hq // 2
+        shape, apart = lam.shape, lam.stride()
+        if shape == (pairs,):
+            shape, apart = (B, tq, pairs), (0, 0, apart[0])
+        if shape != (B, tq, pairs) or lam.dtype is not self._f32 or lam.get_device() != self._device or (apart[2] != 1 and pairs > 1):
+            raise ValueError(f"lam: float32 [{pairs}] or [{B}][{tq}][{pairs}] with dense pairs on {self.state.device} is wanted, got "
+                             f"{lam.dtype} {tuple(lam.shape)} strides {lam.stride()} on {lam.device}")
+        rows, new = (B, tq, Hq, D), (B, tq, H, D)
+        return self._check(self.lib.conf_kv_attend_diff(
+            self.h, layer, tq, lam.data_ptr(), apart[0], apart[1], want("q16", q16, half, rows), want("knew16", knew16, half, new),
+            want("vnew16", vnew16, half, new), want("out16", out16, half, (B, tq, pairs, D)), self._current_stream()), "conf_kv_attend_diff")
 
     def _pages(self, pages_k, pages_v, table):
         """conf_kv_pages of two float16 tensors [pages][page][Hkv][D] and an int32 table [B][pages per sequence]."""

@@ -478,7 +478,7 @@ static size_t table_lds(const conf_kv_handle *h) {
   return h->cv.page_lg ? ((size_t)h->cv.npages * 4 + 15) / 16 * 16 : 0;
 }
 
-static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan, int observe_first = -1, bool shared = false) {
+static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan, int observe_first = -1, AttendKind kind = kAttendPlain) {
   const bool observe = observe_first >= 0;
   const int n_ub = observe ? observe_first + tq : length_bound(h, layer) + tq;     // slots the call sees
   const int W = h->cfg.fp16_window;
@@ -493,7 +493,7 @@ static int plan_for_layer(conf_kv_handle *h, int layer, int tq, AttendPlan *plan
   const bool rows16 = tq > 1 || observe || h->cv.G > 8;
   const int rows = rows16 ? kChunkRows : h->cv.G;
   if (!attend_plan(h->cfg.head_dim, rows, h->cv.chan != 0, h->cv.page_lg != 0, rows16, h->cfg.batch * h->cfg.n_kv_heads, n_ub, n16_ub,
-                   h->forced_splits, h->force_two_launch, table_lds(h), shared, plan))
+                   h->forced_splits, h->force_two_launch, table_lds(h) + (kind == kAttendDiff ? 64 : 0) /* the maps' weights */, kind, plan))
     return CONF_KV_ERR_BAD_SHAPE;
   // the paged layout is read by the single-launch matrix-core kernel only
   if (h->cv.page_lg && (plan->two_launch || !plan->mfma)) return CONF_KV_ERR_BAD_SHAPE;
@@ -508,10 +508,15 @@ static bool prefix_ok(const conf_kv_handle *h, int tq, const conf_kv_prefix *p) 
          on_its_device(h);
 }
 
-// observe_first < 0: append tq tokens and attend, prefix: with a shared prefix in front; >= 0: conf_kv_observe
+struct DiffWeights {
+  const float *lambda;
+  int64_t batch_stride, token_stride;
+};
+// observe_first < 0: append tq tokens and attend, prefix: with a shared prefix in front, diff: rows subtracted in pairs; >= 0: conf_kv_observe
 static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const void *dev_q16,
                          const void *dev_knew16, const void *dev_vnew16, void *dev_out16,
-                         conf_kv_stream stream, int32_t observe_first = -1, const conf_kv_prefix *prefix = nullptr) {
+                         conf_kv_stream stream, int32_t observe_first = -1, const conf_kv_prefix *prefix = nullptr,
+                         const DiffWeights *diff = nullptr) {
   const bool observe = observe_first >= 0;
   if (!h || !dev_q16) return CONF_KV_ERR_INVALID_ARG;
   if (!observe && (!dev_knew16 || !dev_vnew16 || !dev_out16)) return CONF_KV_ERR_INVALID_ARG;
@@ -528,9 +533,15 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
   if (h->appended[layer]) return CONF_KV_ERR_BAD_STATE;
   if (!observe && h->len_ub[layer] + tq > h->cfg.capacity) return CONF_KV_ERR_CAPACITY;
   if (prefix && !prefix_ok(h, tq, prefix)) return CONF_KV_ERR_INVALID_ARG;
+  if (diff) {
+    constexpr int64_t kMostStride = (int64_t)1 << 40;
+    if (!diff->lambda || ((uintptr_t)diff->lambda & 3) || h->cv.G % 2 || tq * h->cv.G > kChunkRows) return CONF_KV_ERR_INVALID_ARG;
+    if (diff->batch_stride < 0 || diff->token_stride < 0 || diff->batch_stride > kMostStride || diff->token_stride > kMostStride) return CONF_KV_ERR_INVALID_ARG;
+    if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
+  }
   const bool shared = prefix && prefix->tokens > 0;
   AttendPlan plan;
-  int rc = plan_for_layer(h, layer, tq, &plan, observe_first, shared);
+  int rc = plan_for_layer(h, layer, tq, &plan, observe_first, shared ? kAttendShared : diff ? kAttendDiff : kAttendPlain);
   if (rc != CONF_KV_OK) return rc;
   [[maybe_unused]] const size_t UPL = (size_t)h->cfg.batch * h->cfg.n_kv_heads;   // phase-trace builds
   AttendLaunch a{};
@@ -599,6 +610,11 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
     a.shared_parts = p.parts;
     a.shared_rows = p.unit_rows;
   }
+  if (diff) {
+    a.lambda = diff->lambda;
+    a.lambda_batch = diff->batch_stride;
+    a.lambda_token = diff->token_stride;
+  }
   CK_HIP(h, launch_attend(h->cv, a, plan, (hipStream_t)stream));
   if (!observe) {
     h->appended[layer] = (uint8_t)tq;
@@ -622,6 +638,12 @@ int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const co
                           const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream) {
   if (!prefix) return CONF_KV_ERR_INVALID_ARG;
   return attend_tokens(h, layer, tq, dev_q16, dev_knew16, dev_vnew16, dev_out16, stream, -1, prefix);
+}
+
+int conf_kv_attend_diff(conf_kv_handle *h, int32_t layer, int32_t tq, const float *dev_lambda, int64_t batch_stride, int64_t token_stride,
+                        const void *dev_q16, const void *dev_knew16, const void *dev_vnew16, void *dev_out16, conf_kv_stream stream) {
+  const DiffWeights diff = {dev_lambda, batch_stride, token_stride};
+  return attend_tokens(h, layer, tq, dev_q16, dev_knew16, dev_vnew16, dev_out16, stream, -1, nullptr, &diff);
 }
 
 int conf_kv_observe(conf_kv_handle *h, int32_t layer, int32_t first, int32_t tq, const void *dev_q16,

@@ -63,9 +63,11 @@ namespace confkv {
 
 static std::atomic<bool> g_use_mfma{true};
 
-static AttendFn attend_fn(AttendForm form, int D, int G, bool chan, bool shared) {
-  return shared ? attend_shared_instance(form, D, G, chan) : attend_instance<false>(form, D, G, chan);
+static AttendFn attend_fn(AttendForm form, int D, int G, bool chan, AttendKind kind) {
+  return kind == kAttendShared ? attend_shared_instance(form, D, G, chan) : kind == kAttendDiff ? attend_diff_instance(form, D, G, chan)
+                                                                                                : attend_instance<false>(form, D, G, chan);
 }
+static AttendKind attend_kind(const AttendLaunch &a) { return a.lambda ? kAttendDiff : a.shared_parts > 0 ? kAttendShared : kAttendPlain; }
 
 // Second launch of the two-launch form.
 static AttendFn attend_fn_finish(int D, int G) {
@@ -170,12 +172,12 @@ static int attend_occupancy(AttendFn fn, size_t lds) {
 }
 
 bool attend_plan(int D, int G, bool chan, bool paged, bool chunk, int units_per_layer, int n_ub, int n16_ub, int forced_splits,
-                 bool force_two_launch, size_t extra_lds, bool shared, AttendPlan *plan) {
+                 bool force_two_launch, size_t extra_lds, AttendKind kind, AttendPlan *plan) {
   const DeviceLimits &lim = device_limits();
   if (!lim.ok) return false;
   if (attend_instance<false>(chunk ? kFormMfma : kFormValu, D, G, chunk && chan) == nullptr) return false;
   const bool mfma = chunk || wants_mfma(D, G, n16_ub < n_ub);
-  AttendFn fn = attend_fn(!mfma ? kFormValu : paged ? kFormPaged : kFormMfma, D, G, chan, shared);
+  AttendFn fn = attend_fn(!mfma ? kFormValu : paged ? kFormPaged : kFormMfma, D, G, chan, kind);
   if (!fn) return false;
   const long long nv = (long long)n_ub + n16_ub;
   // One workgroup per CU measured best: the exchange between the splits of a unit (statistics
@@ -232,7 +234,7 @@ bool attend_plan(int D, int G, bool chan, bool paged, bool chunk, int units_per_
     S = (S + 255) / 256 * 256;
     const size_t lds = attend_lds_bytes(D, G, 0, mfma) + extra_lds;
     if (lds > lim.max_lds) return false;
-    if (lds > 64 * 1024) (void)attend_occupancy(attend_fn(kFormMfmaSpill, D, G, chan, shared), lds);   // raises the dynamic-LDS limit
+    if (lds > 64 * 1024) (void)attend_occupancy(attend_fn(kFormMfmaSpill, D, G, chan, kind), lds);   // raises the dynamic-LDS limit
     plan->splits = ns;
     plan->stash_tokens = S;
     plan->lds_bytes = lds;
@@ -318,8 +320,8 @@ hipError_t launch_attend(const CacheView &cv, const AttendLaunch &a_in, const At
     const bool rows16 = a.tq > 1 || a.observe_first >= 0 || cv.G > 8;
     const int rows2 = rows16 ? kChunkRows : cv.G;                   // query rows per unit
     if (rows16 && !plan.mfma) return hipErrorInvalidValue;
-    AttendFn first = attend_fn(plan.mfma ? kFormMfmaSpill : kFormValuSpill, cv.D, plan.mfma ? rows2 : cv.G, cv.chan != 0, a.shared_parts > 0);
-    AttendFn second = plan.mfma && cv.D == 64 ? attend_fn_finish_padded(rows2) : attend_fn_finish(cv.D, rows2);
+    AttendFn first = attend_fn(plan.mfma ? kFormMfmaSpill : kFormValuSpill, cv.D, plan.mfma ? rows2 : cv.G, cv.chan != 0, attend_kind(a));
+    AttendFn second = a.lambda ? attend_diff_finish(cv.D, rows2) : plan.mfma && cv.D == 64 ? attend_fn_finish_padded(rows2) : attend_fn_finish(cv.D, rows2);
     if (!first || !second || !a.spill) return hipErrorInvalidValue;
     hipLaunchKernelGGL(first, grid, dim3(kAttThreads), plan.lds_bytes, stream, cv.len, cv.n8, cv.head16, cv.head8, a.layer * cv.B * cv.Hkv, cv.Hkv, a.kv_major, cv, a, plan.splits,
                        plan.stash_tokens);
@@ -329,7 +331,7 @@ hipError_t launch_attend(const CacheView &cv, const AttendLaunch &a_in, const At
     return hipGetLastError();
   }
   if (plan.wide_groups) {
-    if (a.shared_parts > 0) return hipErrorInvalidValue;      // (the caller has refused it)
+    if (attend_kind(a) != kAttendPlain) return hipErrorInvalidValue;      // (the caller has refused it)
     a.dbg = nullptr;
     a.max_splits = wide_max_splits(plan.wide_groups * kWideRows);
     hipLaunchKernelGGL(attend_fn_wide(plan.wide_groups, plan.wide_kept), grid, dim3(kAttThreads), plan.lds_bytes, stream, cv.len, cv.n8, cv.head16, cv.head8, a.layer * cv.B * cv.Hkv, cv.Hkv, a.kv_major, cv, a, plan.splits, 0);
@@ -338,7 +340,7 @@ hipError_t launch_attend(const CacheView &cv, const AttendLaunch &a_in, const At
   const bool rows16 = a.tq > 1 || a.observe_first >= 0 || cv.G > 8;
   const int rows = rows16 ? kChunkRows : cv.G;
   if (rows16 && !plan.mfma) return hipErrorInvalidValue;
-  AttendFn fn = attend_fn(!plan.mfma ? kFormValu : cv.page_lg ? kFormPaged : kFormMfma, cv.D, plan.mfma ? rows : cv.G, cv.chan != 0, a.shared_parts > 0);
+  AttendFn fn = attend_fn(!plan.mfma ? kFormValu : cv.page_lg ? kFormPaged : kFormMfma, cv.D, plan.mfma ? rows : cv.G, cv.chan != 0, attend_kind(a));
   if (!fn) return hipErrorInvalidValue;
 #ifdef CONFKV_TRACE
   if (a.dbg && plan.mfma) {             // time stamps live in LDS behind the kernel's own

@@ -671,6 +671,29 @@ __device__ __forceinline__ void request_ema(const CacheView &cv, const Slice &sl
 }
 
 // ---------------------------------------------------------------------------------------
+// Differential attention (conf_kv_attend_diff): rows 2 j and 2 j + 1 of a unit are the two maps of pair j, whose output is
+//   sum_i (p_i - lambda_j p'_i) V_i = O / L - lambda_j O' / L'
+// The maps run as any two rows do; what is theirs is the end: an output element takes both rows' partials, and a slot's
+// importance is the size of the weight its value had, sum_j |p_i - lambda_j p'_i|.  The weights, eight at most, wait in LDS.
+__device__ __forceinline__ float *diff_weights() {
+  __shared__ float s_lambda[kChunkRows / 2];
+  return s_lambda;
+}
+// thread j's weight (requested with the first rows, stored in front of a barrier that the epilogue is behind)
+__device__ __forceinline__ float request_diff_weight(const CacheView &cv, const AttendLaunch &a, int rows, int tq, int gq) {
+  const int r = 2 * (int)threadIdx.x, t = r / gq;
+  if (r >= rows || t >= tq) return 0.f;
+  return a.lambda[blockIdx.z * a.lambda_batch + t * a.lambda_token + kv_head_index(a) * (gq >> 1) + ((r - t * gq) >> 1)];
+}
+// Where channel d of pair j goes in [B][tq][Hq / 2][D].
+template <bool kRows>
+__device__ __forceinline__ size_t diff_out_index(const CacheView &cv, const AttendLaunch &a, const Slice &sl, int tq, int gq, int j, int d,
+                                                 int D) {
+  const int t = kRows ? token_of_row(a, 2 * j) : 0, half = gq >> 1;
+  return ((((size_t)sl.b * tq + t) * cv.Hkv + sl.g) * half + (j - t * half)) * D + d;
+}
+
+// ---------------------------------------------------------------------------------------
 // Epilogue shared by both bodies (kShared: with a shared prefix's partial results among the wavefronts').  On entry wm/wl/wo hold NP per-wavefront partials
 // (after a workgroup barrier): partial k is [G][D] floats, rows DS apart, at
 // wo + (k % kAttWaves) * WSTR + (k / kAttWaves) * G * DS; stash holds the slice's raw scores.
@@ -679,7 +702,7 @@ __device__ __forceinline__ void request_ema(const CacheView &cv, const Slice &sl
 // later launch, which needs no wait (wm/wl are unused and wo holds the [G][gs] weights) --
 // the pair serves shapes whose splits cannot all be resident at once.
 // ---------------------------------------------------------------------------------------
-template <int D, int G, int NP, int WSTR, int kPhase = 0, int DR = D, int DS = D, bool kPaged = false, bool kShared = false>
+template <int D, int G, int NP, int WSTR, int kPhase = 0, int DR = D, int DS = D, bool kPaged = false, bool kShared = false, bool kDiff = false>
 __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const AttendLaunch &a,
                                                 const Slice &sl, int ns, int S, float *stash,
                                                 float *wm, float *wl, float *wo, float *gm,
@@ -748,10 +771,33 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
   // workgroup merge of the per-wavefront output partials: kEPT channels per thread, each
   // published as a word that carries the launch's epoch, so that nobody has to wait for the
   // stores to land before announcing them
+  [[maybe_unused]] const float *lambda = kDiff ? diff_weights() : nullptr;
+  if constexpr (kDiff && kPhase == 0) {
+    // a single split: both rows of a pair meet here, an element per thread and turn
+    for (int idx = tid; !exchange && idx < G / 2 * D; idx += kAttThreads) {
+      const int j = __builtin_amdgcn_readfirstlane(idx / D), d = idx - j * D;   // (a wavefront's elements belong to one pair)
+      double y[2];
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const int h = 2 * j + k2, r8 = (h & 7) * 8;
+        const bool low = HB == 1 || h < 8;
+        const float pw = low ? part_w[0] : part_w[HB - 1];
+        float o = 0.f;
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          const float f = lane_f(pw, r8 + k), v = wo[k * WSTR + h * DS + d];
+          o = __float_as_int(f) != 0 ? fmaf(v, f, o) : o;
+        }
+        y[k2] = (double)o * lane_d(low ? row_inv[0] : row_inv[HB - 1], r8);
+      }
+      if (2 * j < tq * gq && d < DR)
+        a.out[diff_out_index<(G > 8)>(cv, a, sl, tq, gq, j, d, DR)] = half_of_double(y[0] - (double)lambda[j] * y[1]);
+    }
+  }
   constexpr int kEPT = G * D > kAttThreads ? 2 : 1;
   constexpr int kMerge = (G * D + kEPT * kAttThreads - 1) / (kEPT * kAttThreads);
   static_assert(D % (kEPT * kWave) == 0, "a wavefront's elements belong to one row");
-  if (kPhase != 2) {
+  if (kPhase != 2 && (!kDiff || exchange)) {
 #pragma unroll
     for (int p = 0; p < kMerge; ++p) {
       const int idx = kEPT * (tid + p * kAttThreads);
@@ -811,14 +857,17 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
   // together, and an element's address, sum and store come once (16 rows, four splits: 0.9 us from the request to the
   // store; a pass per kOut-th element with a lane per split took 1.8).
   constexpr int kOutLg = G > 8 ? 2 : G > 4 ? 1 : 0, kOut = 1 << kOutLg;
-  const int per = (int)div_splits(a, G * D + ns - 1);
+  constexpr int kMaps = kDiff ? 2 : 1, kOutRows = G / kMaps;   // rows that make up an output row
+  const int per = (int)div_splits(a, kOutRows * D + ns - 1);
   const int lgl = max(lg - kOutLg, 0);               // log2(lanes)
   const int epp = kAttThreads >> lgl;                // output elements per pass over the workgroup
   const int sub = tid & ((1 << lgl) - 1), oe = tid >> lgl;   // this thread's first split and element within a pass
-  unsigned long long opre[kOut];
+  unsigned long long opre[kMaps * kOut];
   auto out_word = [&](int p, int q) {                // of pass p: the q-th word, or the unit's first where there is none
-    const int os = sub + (q << lgl), i = p * epp + oe, e = sl.j * per + i;
-    return &pou[os < ns && i < per && e < G * D ? (size_t)os * G * D + e : 0];
+    const int os = sub + ((q & (kOut - 1)) << lgl), i = p * epp + oe, e = sl.j * per + i;
+    // (two maps: the first row's words, then the second's)
+    const int at = kDiff ? e + (e / D + q / kOut) * D : e;
+    return &pou[os < ns && i < per && e < kOutRows * D ? (size_t)os * G * D + at : 0];
   };
   const unsigned tag = tag_of(a);
   __shared__ int s_ok;
@@ -864,7 +913,7 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
     }
     // the output partials are requested now and used behind the importance arithmetic
 #pragma unroll
-    for (int q = 0; q < kOut; ++q) opre[q] = ld_tagged(out_word(0, q));
+    for (int q = 0; q < kMaps * kOut; ++q) opre[q] = ld_tagged(out_word(0, q));
 #pragma unroll
     for (int h = 0; h < G; ++h) { g_m[h] = gm[h]; g_w[h] = ginv[G + h]; }
   } else {
@@ -879,16 +928,17 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
   auto finish_output = [&]() {
     for (int p = 0; p * epp < per; ++p) {
       const int i = p * epp + oe, e = sl.j * per + i;                // element of the [G][D] output
-      const bool mine = i < per && e < G * D;
+      const bool mine = i < per && e < kOutRows * D;
       if (p > 0) {
 #pragma unroll
-        for (int q = 0; q < kOut; ++q) opre[q] = ld_tagged(out_word(p, q));
+        for (int q = 0; q < kMaps * kOut; ++q) opre[q] = ld_tagged(out_word(p, q));
       }
       // a word that is not this launch's yet is asked for again (bounded)
       auto all_here = [&]() {
         bool here = true;
 #pragma unroll
-        for (int q = 0; q < kOut; ++q) here &= !mine || sub + (q << lgl) >= ns || (unsigned)(opre[q] >> 32) == tag;
+        for (int q = 0; q < kMaps * kOut; ++q)
+          here &= !mine || sub + ((q & (kOut - 1)) << lgl) >= ns || (unsigned)(opre[q] >> 32) == tag;
         return here;
       };
       bool here = all_here();
@@ -897,7 +947,7 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
         __builtin_amdgcn_s_sleep(1);
         if (!here) {
 #pragma unroll
-          for (int q = 0; q < kOut; ++q) opre[q] = ld_tagged(out_word(p, q));
+          for (int q = 0; q < kMaps * kOut; ++q) opre[q] = ld_tagged(out_word(p, q));
           here = all_here();
         }
       }
@@ -906,14 +956,21 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
         if ((tid & 63) == __builtin_ctzll(missing)) atomicAdd(&cv.stats[kStatDeviceErr], 1ull);
         continue;
       }
-      const int h = mine ? e / D : 0;
+      const int h = mine ? e / D * kMaps : 0;
       float c = 0.f;
+      [[maybe_unused]] float c2 = 0.f;
 #pragma unroll
-      for (int q = 0; q < kOut; ++q) {
-        const int os = sub + (q << lgl);
-        const float wgt = mine && os < ns ? pml[(h << lg) + os] : 0.f;   // e^{m_s - M} / L of that split and row
+      for (int q = 0; q < kMaps * kOut; ++q) {
+        const int os = sub + ((q & (kOut - 1)) << lgl);
+        const float wgt = mine && os < ns ? pml[((h + q / kOut) << lg) + os] : 0.f;   // e^{m_s - M} / L of that split and row
         // (an empty partial may hold anything; a weight that is NaN, from a score that is none, must show)
-        c += wgt != 0.f ? __uint_as_float((unsigned)opre[q]) * wgt : 0.f;
+        (q < kOut ? c : c2) += wgt != 0.f ? __uint_as_float((unsigned)opre[q]) * wgt : 0.f;
+      }
+      if constexpr (kDiff) {
+        c = group_sum(fmaf(-lambda[h / 2], c2, c), 1 << lgl);
+        const int d = e - h / 2 * D;
+        if (mine && sub == 0 && h < tq * gq && d < DR) a.out[diff_out_index<(G > 8)>(cv, a, sl, tq, gq, h / 2, d, DR)] = __float2half_rn(c);
+        continue;
       }
       c = group_sum(c, 1 << lgl);
       if (mine && sub == 0 && h < tq * gq && a.out && e - h * D < DR)
@@ -929,14 +986,27 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
   // The new values of the first kPre slots per thread stay in registers until the output is
   // out: a store between the request of the output partials and their use would make that use
   // wait for the store's acknowledgement as well (loads and stores share one in-order counter).
+  // a slot's weight in the output, over all rows
+  auto mass_of = [&](int t) {
+    double A = 0.0;
+    if constexpr (kDiff) {
+#pragma unroll
+      for (int h = 0; h < G; h += 2) {
+        const double p = (double)exp_nonpos(stash[h * S + t] - g_m[h]) * g_w[h];
+        A += fabs(p - (double)lambda[h / 2] * ((double)exp_nonpos(stash[(h + 1) * S + t] - g_m[h + 1]) * g_w[h + 1]));
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < G; ++h) A += (double)exp_nonpos(stash[h * S + t] - g_m[h]) * g_w[h];
+    }
+    return A;
+  };
   float ema_new[kPre + 1];
 #pragma unroll
   for (int k = 0; k < kPre; ++k) {
     const int t = tid + k * kAttThreads;
     if (t < sl.ntok) {
-      double A = 0.0;
-#pragma unroll
-      for (int h = 0; h < G; ++h) A += (double)exp_nonpos(stash[h * S + t] - g_m[h]) * g_w[h];
+      const double A = mass_of(t);
       const double old = (sl.slot_of(t) >= first_new) ? 0.0 : (double)ema_old[k];   // a new token starts at 0
       ema_new[k] = (float)(lam * old + oml * A);
       if (!exchange) EMA[ema_row(t)] = ema_new[k];
@@ -968,9 +1038,7 @@ __device__ __forceinline__ void attend_epilogue(const CacheView &cv, const Atten
     for (int k = 0; k < kBatch; ++k) {
       const int t = t0 + k * kAttThreads;
       if (t < sl.ntok) {
-        double A = 0.0;
-#pragma unroll
-        for (int h = 0; h < G; ++h) A += (double)exp_nonpos(stash[h * S + t] - g_m[h]) * g_w[h];
+        const double A = mass_of(t);
         const double prev = (sl.slot_of(t) >= first_new) ? 0.0 : (double)old[k];   // a new token starts at 0
         EMA[row[k]] = (float)(lam * prev + oml * A);
       }
@@ -1053,7 +1121,7 @@ __global__ __launch_bounds__(kAttThreads) void attend_kernel(const int32_t *w_le
 
 // Second launch of the two-launch form: same grid; merges the published partials of the unit,
 // updates the EMA of its slice from the spilled scores and normalises its share of the output.
-template <int D, int G, int DR = D>
+template <int D, int G, int DR = D, bool kDiff = false>
 __global__ __launch_bounds__(kAttThreads) void attend_finish_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t *w_h16, const int32_t *w_h8, int w_unit0, int w_hkv, int w_kvm, CacheView cv, AttendLaunch a_in, int ns,
                                                                     int S) {
   const AttendLaunch a = resolve_launch(cv, a_in);
@@ -1064,7 +1132,11 @@ __global__ __launch_bounds__(kAttThreads) void attend_finish_kernel(const int32_
   const Slice sl = make_slice(cv, a, ns, S);
   float *stash = a.spill + ((size_t)unit_in_layer(cv, a) * ns + split_index(a)) * G * S;
   float unused[kEmaAhead];
-  attend_epilogue<D, G, 1, 0, 2, DR>(cv, a, sl, ns, S, stash, nullptr, nullptr, pml, gm, ginv, unused);
+  if constexpr (kDiff) {                        // (the epilogue's first barrier is in front of their use)
+    const float weight = request_diff_weight(cv, a, G, G > 8 ? a.tq : 1, G > 8 ? a.gq : G);
+    if (threadIdx.x < kChunkRows / 2) diff_weights()[threadIdx.x] = weight;
+  }
+  attend_epilogue<D, G, 1, 0, 2, DR, D, false, false, kDiff>(cv, a, sl, ns, S, stash, nullptr, nullptr, pml, gm, ginv, unused);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1337,7 +1409,7 @@ __device__ __forceinline__ void reload_far_item(const TileSource &t, const Slice
 //    register transpose before took 32 byte permutes and 16 stores per INT8 tile);
 //  - the output is formed transposed, [channel][row], so a lane holds four neighbouring channels of one row and a
 //    wavefront's partial leaves in eight 16-byte stores.
-template <int G, bool kChan = false, bool kSpill = false, int DR = 128, bool kPaged = false, bool kShared = false>
+template <int G, bool kChan = false, bool kSpill = false, int DR = 128, bool kPaged = false, bool kShared = false, bool kDiff = false>
 __global__ __launch_bounds__(kAttThreads)
 __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attend_mfma_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t *w_h16, const int32_t *w_h8, int w_unit0, int w_hkv, int w_kvm, CacheView cv, AttendLaunch a_in, int ns, int S) {
@@ -1451,6 +1523,8 @@ void attend_mfma_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t
     new_piece = *(const int4 *)((r4 ? a.vnew : a.knew) + ((size_t)sl.b * cv.Hkv + sl.g) * DR + (c16 & (DR / 8 - 1)) * 8);
   float ema_old[kEmaAhead];
   if (!kSpill) request_ema<kPaged>(cv, sl, ema_old);
+  [[maybe_unused]] float diff_weight = 0.f;
+  if constexpr (kDiff && !kSpill) diff_weight = request_diff_weight(cv, a, G, tq, gq);
   TS(3);
   append_new_token<DR, kPaged>(cv, a, sl, ns, tq);
   const float NEG = -INFINITY;
@@ -1847,10 +1921,12 @@ void attend_mfma_kernel(const int32_t *w_len, const int32_t *w_n8, const int32_t
           make_float4(O[nt][0] - bias, O[nt][1] - bias, O[nt][2] - bias, O[nt][3] - bias);
   }
 
+  if constexpr (kDiff && !kSpill)
+    if (tid < kChunkRows / 2) diff_weights()[tid] = diff_weight;
   TS(17);
   __syncthreads();
   TS(18);
-  attend_epilogue<D, G, NP, kTileBytes / 4, kSpill ? 1 : 0, DR, kPartRow, kPaged, kShared>(cv, a, sl, ns, SS, stash, wm, wl, wo, gm, ginv, ema_old);
+  attend_epilogue<D, G, NP, kTileBytes / 4, kSpill ? 1 : 0, DR, kPartRow, kPaged, kShared, kDiff>(cv, a, sl, ns, SS, stash, wm, wl, wo, gm, ginv, ema_old);
   TS_DUMP();
 }
 
@@ -1897,6 +1973,10 @@ AttendFn attend_instance(AttendForm form, int D, int G, bool chan) {
                 : (AttendFn)attend_mfma_kernel<kChunkRows, false, true, 128, false, kShared>;
   return nullptr;
 }
+// those of differential attention (attend_diff.hip)
+AttendFn attend_diff_instance(AttendForm form, int D, int G, bool chan);
+// and the second launch behind their kFormMfmaSpill
+AttendFn attend_diff_finish(int D, int G);
 // those that take in a shared prefix (attend_join.hip)
 AttendFn attend_shared_instance(AttendForm form, int D, int G, bool chan);
 

@@ -108,7 +108,12 @@ struct AttendLaunch {
   const float2 *shared_ml; // [units per layer][parts][rows] maximum and normaliser
   const float *shared_o;   // [units per layer][parts][rows][D]
   int shared_parts, shared_rows;
+  // differential attention: weights [B][tq][Hkv * gq / 2] of the second maps, sequences and tokens so far apart (else null)
+  const float *lambda;
+  long long lambda_batch, lambda_token;
 };
+// Which of the kernels' kinds: as they are, with a shared prefix's partial results taken in, with rows subtracted in pairs.
+enum AttendKind { kAttendPlain, kAttendShared, kAttendDiff };
 constexpr int kAttendMaxSplits = 64;
 constexpr int kChunkRows = 16;     // query rows per unit of a multi-token call (one matrix-core tile)
 // Multiplier and shift of a division by ns (2 .. 64): x / ns = (high word of x * multiplier) >> shift for all 0 <= x < 2^31.
@@ -120,7 +125,7 @@ size_t attend_spill_floats(int units_per_layer, int G, int cap);   // scratch th
 // a multi-token call, which only has the single-launch matrix-core form).  Returns false when no plan fits the device.
 // extra_lds: bytes the launch needs behind the kernel's own dynamic LDS (the block table of the paged layout).
 bool attend_plan(int D, int G, bool chan, bool paged, bool chunk, int units_per_layer, int n_ub, int n16_ub, int forced_splits,
-                 bool force_two_launch, size_t extra_lds, bool shared /* a shared prefix is taken in */, AttendPlan *plan);
+                 bool force_two_launch, size_t extra_lds, AttendKind kind, AttendPlan *plan);
 // Plan of a call with more than kChunkRows query rows per unit (at most kWideRowsMax); false when
 // the shape cannot be served.  major_kv: kv-heads of the kv-head-first grid, 0 for the other.
 // n_ub: the most slots of a unit; n16_least, n16_ub: the fewest and the most FP16 ones.
