@@ -159,13 +159,13 @@ struct PgSource {
   }
   // the table's entry for a token (a place behind the table: its last entry; nothing read from there counts)
   __device__ __forceinline__ int entry(int token) const { return table[min(token >> lg, max_pages - 1)]; }
-  // Offset of the lane's piece of the RWI rows from token r0 on (a multiple of RWI; so they lie in one page, whose entry is e).
-  __device__ __forceinline__ long long offset(int r0, int e) const {
+  // Offset of token r0's row (a multiple of RWI, as are the pages' lengths: the next RWI lie in one page, whose entry is e).
+  __device__ __forceinline__ long long page_offset(int r0, int e) const {
     e = min(max(e, 0), n_pages - 1);
-    return e * page_stride + (r0 & ((1 << lg) - 1)) * token_stride + lane_off;
+    return e * page_stride + (r0 & ((1 << lg) - 1)) * token_stride;
   }
   __device__ __forceinline__ void load(int r0, int e, int4 &kr, int4 &vr) const {
-    const long long o = offset(r0, e);
+    const long long o = page_offset(r0, e) + lane_off;
     const __half *kp = k + o, *vp = v + o;
     if (r0 + RWI > c) {                                // (tokens of the call among them; behind the last one its row again)
       const int lane = threadIdx.x & 63, t = min(r0 + lane / PR, n - 1);
@@ -235,10 +235,12 @@ struct PgRows {
     }
   }
   // scores of keys key0 .. key0 + 31 -> probabilities; element i: key key0 + 8 (i / 4) + 4 h + i % 4
+  // (kMask: some may be behind what a row sees)
+  template <bool kMask>
   __device__ __forceinline__ void weigh(pg_f16 &sc, int key0, float c, pg_h8 (&pb)[2]) {
     const int h = (threadIdx.x & 63) >> 5;
     const float NEG = -INFINITY;
-    if (key0 + kPgKeys > least) {
+    if (kMask && key0 + kPgKeys > least) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + (i & 3) < lim - key0 - 4 * h ? sc[i] : NEG;
     }
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     pg_f16 sc;
     pg_h8 pb[2];
     st.template scores<L::KROW>(Kt, sc);
-    st.weigh(sc, key0, c, pb);
+    st.template weigh<true>(sc, key0, c, pb);
     st.template add<L::VROW>(Vt, pb);
     pg_wave_sync();
   }
@@ -520,18 +522,82 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 }
 
 // ---------------------------------------------------------------------------------------
-// More rows: bound by the matrix products and the exponentials.  Four wavefronts of 32 * RB rows each share tiles of 64 keys in LDS,
-// two buffers, one barrier per tile; the tile after the next is in flight in registers.
+// More rows: bound by the matrix products and the exponentials.  Four wavefronts of 32 * RB rows each share tiles of 64 keys.
+//
+// Rows come straight into LDS (16 bytes a lane, no registers on the way), so a tile's rows lie as they are, 2 D bytes apart, and the
+// pieces of a row are permuted instead: piece p of row r lies at slot p ^ f(r), with an f that puts what the reads below take
+// together on different banks -- eight lanes' pieces of K at one place of their rows, the pieces of four neighbouring V rows.
 // ---------------------------------------------------------------------------------------
 constexpr int kManyWaves = 4, kManyKeys = 64, kManyThreads = kManyWaves * kWave;
 
+template <int D>
+__device__ __forceinline__ constexpr int pg_swizzle(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+// Sixteen bytes per lane from the lane's address to LDS bytes [to, to + 1024), lane by lane.
+__device__ __forceinline__ void pg_load_lds(const void *from, unsigned to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ unsigned pg_lds_at(const void *p) {
+  return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
+}
+// Everything the wavefront has requested is there, and then everybody's.
+__device__ __forceinline__ void pg_arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void pg_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+template <int D, int RB>
+struct PgMany {
+  static constexpr int PR = D / 8, RWI = kWave / PR, RPP = kManyThreads / PR, NP = kManyKeys / RPP, ROW = 2 * D;
+  static constexpr int R = kManyWaves * RB * kPgRows;
+  static constexpr int kPlane = kManyKeys * ROW, kBuffer = 2 * kPlane, kBuffers = RB == 1 ? 2 : 3;
+
+  PgRows<D> st[RB];
+  float c;
+  int k_off, v_off;                                    // the lane's places in a tile: K fragment 0, V fragment 0
+
+  __device__ __forceinline__ void init(const PagesLaunch &a, const PgJob &j, int first_row) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, t16 = lane & 15, c2 = (lane >> 4) & 1;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) st[rb].init(a, j, first_row + (w * RB + rb) * kPgRows);
+    c = a.sm_scale * 1.44269504088896341f;
+    k_off = l32 * ROW + ((h ^ pg_swizzle<D>(l32)) << 4);
+    const int vr = 4 * h + (t16 >> 2);
+    v_off = kPlane + vr * ROW + (((2 * c2 + ((t16 & 3) >> 1)) ^ pg_swizzle<D>(vr)) << 4) + 8 * (t16 & 1);
+  }
+  // scores of the 32 keys at byte offset `at`
+  __device__ __forceinline__ void scores(const uint8_t *lds, int at, pg_f16 (&sc)[RB]) const {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[rb][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const pg_h8 kf = *(const pg_h8 *)(lds + at + (k_off ^ (s << 5)));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, st[rb].qf[s], sc[rb], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void add(const uint8_t *lds, int at, const pg_h8 (&pb)[RB][2]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int nt = 0; nt < D / 32; ++nt) {
+        const uint8_t *vp = lds + at + 16 * s * ROW;
+        const pg_h4 v0 = pg_read_tr(vp + (v_off ^ (nt << 6))), v1 = pg_read_tr(vp + 8 * ROW + (v_off ^ (nt << 6) ^ 32));
+        const pg_h8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) st[rb].O[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pb[rb][s], st[rb].O[nt], 0, 0, 0);
+      }
+  }
+};
+
 template <int D, int RB>
 __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB == 1 ? 2 : 1, RB == 1 ? 2 : 1))) void pages_many_kernel(PagesLaunch a) {
-  using L = PgTile<D>;
-  constexpr int PR = D / 8, RWI = kWave / PR, RPP = kManyThreads / PR, NP = kManyKeys / RPP, R = kManyWaves * RB * kPgRows;
-  constexpr int kKBytes = kManyKeys * L::KROW, kBuffer = 2 * L::kBytes;
-  __shared__ __align__(16) uint8_t s_tile[2 * kBuffer];
-  __shared__ int s_bad[2];
+  using M = PgMany<D, RB>;
+  constexpr int PR = M::PR, RWI = M::RWI, RPP = M::RPP, NP = M::NP, R = M::R, ROW = M::ROW;
+  __shared__ __align__(16) uint8_t s_tile[M::kBuffers * M::kBuffer];
+  __shared__ int s_bad[M::kBuffers];
+  static_assert(kManyWaves * kPgRows * D * 4 <= sizeof(s_tile), "the wavefronts' rows fit the tiles' room");
   PgJob j;
   if (!pg_job(a, R, kManyQuantum, blockIdx.x, j)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -541,90 +607,116 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB
   const int lo = j.part_keys == kNoSplit ? 0 : j.part * j.part_keys;
   const int seen = j.q.c + last_row / a.G + 1;           // keys that the block's last row sees
   const int hi = (int)min((long long)lo + j.part_keys, (long long)seen);
-  const int all_least = j.q.c + first_row / a.G + 1;
-  struct Turn { int4 k[NP], v[NP]; } x;
-  auto load = [&](int base, int ent) {
+  const int all_least = j.q.c + first_row / a.G + 1;     // and its first one
+  const int tiles = hi > lo ? (hi - lo + kManyKeys - 1) / kManyKeys : 0;
+  const int full = max(0, (min(all_least, hi) - lo) / kManyKeys);   // tiles that every row sees to the end
+  // The lane's row and piece of a wavefront's load; f does not depend on which of a tile's loads it is.
+  const int lrow = RWI * w + lane / PR, lpiece = (lane % PR) ^ pg_swizzle<D>(lrow);
+  const long long lane_off = (lane / PR) * src.token_stride + lpiece * 8;
+  const unsigned lds0 = pg_lds_at(s_tile);
+  int ent = src.entry(lo + lane);
+  auto issue = [&](int t, int buffer) {                  // (every tile's entries were requested with the tile before)
+    if (t >= tiles) return;
+    const int base = lo + t * kManyKeys;
+    const unsigned to = lds0 + buffer * M::kBuffer + RWI * w * ROW;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = RPP * i + RWI * w;
-      src.load(base + r, __builtin_amdgcn_readlane(ent, r), x.k[i], x.v[i]);
-    }
-  };
-  int ent = src.entry(lo + lane);
-  if (lo < hi) {
-    load(lo, ent);
-    ent = src.entry(lo + kManyKeys + lane);
-  }
-  PgRows<D> st[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) st[rb].init(a, j, first_row + (w * RB + rb) * kPgRows);
-  const float c = a.sm_scale * 1.44269504088896341f;
-  // (see pages_few_kernel)
-  auto store = [&](int turn, int base) {
-    if (base + kManyKeys > all_least) {
-      unsigned odd = 0u;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) odd |= pg_odd_piece(x.v[i]);
-      if (__builtin_expect(odd != 0u, 0)) {
-        s_bad[turn & 1] = turn;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) pg_drop_odd(x.v[i]);
-      }
-    }
-    uint8_t *Kt = s_tile + (turn & 1) * kBuffer, *Vt = Kt + kKBytes;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int row = tid / PR + RPP * i;
-      *(int4 *)(Kt + row * L::KROW + tid % PR * 16) = x.k[i];
-      *(int4 *)(Vt + row * L::VROW + tid % PR * 16) = x.v[i];
-    }
-  };
-  if (tid < 2) s_bad[tid] = -1;
-  __syncthreads();
-  bool dropped = false;
-  if (lo < hi) {
-    store(0, lo);
-    if (lo + kManyKeys < hi) {
-      load(lo + kManyKeys, ent);
-      ent = src.entry(lo + 2 * kManyKeys + lane);
-    }
-  }
-  __syncthreads();
-  int turn = 0;
-  for (int base = lo; base < hi; base += kManyKeys, ++turn) {
-    if (base + kManyKeys < hi) store(turn + 1, base + kManyKeys);
-    if (base + 2 * kManyKeys < hi) {
-      load(base + 2 * kManyKeys, ent);
-      ent = src.entry(base + 3 * kManyKeys + lane);
-    }
-    const uint8_t *Kt = s_tile + (turn & 1) * kBuffer, *Vt = Kt + kKBytes;
-    dropped |= s_bad[turn & 1] == turn;
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const int key0 = base + sub * kPgKeys;
-      {
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          if (key0 >= min(hi, st[rb].most)) continue;
-          pg_f16 sc;
-          pg_h8 pb[2];
-          st[rb].template scores<L::KROW>(Kt + sub * kPgKeys * L::KROW, sc);
-          st[rb].weigh(sc, key0, c, pb);
-          st[rb].template add<L::VROW>(Vt + sub * kPgKeys * L::VROW, pb);
+      const long long o = src.page_offset(base + r, __builtin_amdgcn_readlane(ent, r)) + lane_off;
+      const __half *kp = src.k + o, *vp = src.v + o;
+      if (base + r + RWI > src.c) {                      // tokens of the call among them
+        const int token = min(base + RPP * i + lrow, src.n - 1);
+        if (token >= src.c) {
+          const long long m = (token - src.c) * src.new_stride + lpiece * 8;
+          kp = src.knew + m;
+          vp = src.vnew + m;
         }
       }
+      pg_load_lds(kp, to + RPP * i * ROW);
+      pg_load_lds(vp, to + M::kPlane + RPP * i * ROW);
     }
-    __syncthreads();
+    if (t + 1 < tiles) ent = src.entry(base + kManyKeys + lane);
+  };
+  if (tid < M::kBuffers) s_bad[tid] = -1;
+  issue(0, 0);
+  M st;
+  st.init(a, j, first_row);
+  if (M::kBuffers > 2) issue(1, 1);
+  __syncthreads();
+  bool dropped = false;
+  // Values of keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN one: where
+  // there are such rows these values leave the tile, by the hand of the lane that brought them, and reach the rows that do see
+  // them at the end.
+  auto scrub = [&](int t, int buffer) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      int4 *p = (int4 *)(s_tile + buffer * M::kBuffer + M::kPlane + (RPP * i + RWI * w) * ROW + lane * 16);
+      int4 v = *p;
+      if (__builtin_expect(pg_odd_piece(v) != 0u, 0)) {
+        s_bad[buffer] = t;
+        pg_drop_odd(v);
+        *p = v;
+      }
+    }
+  };
+  int buffer = 0;
+  auto next_buffer = [&](int b) { return b + 1 == M::kBuffers ? 0 : b + 1; };
+  auto turn = [&](int t, bool tail) {                    // tile t is there, and the next one but kBuffers - 2 is requested
+    pg_arrive();
+    if (tail) {
+      scrub(t, buffer);
+      pg_arrive();
+    }
+    pg_barrier();
+    issue(t + M::kBuffers - 1, buffer == 0 ? M::kBuffers - 1 : buffer - 1);
+  };
+  int t = 0;
+  for (; t < full; ++t, buffer = next_buffer(buffer)) {
+    turn(t, false);
+    const int at = buffer * M::kBuffer;
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      pg_f16 sc[RB];
+      pg_h8 pb[RB][2];
+      st.scores(s_tile, at + sub * kPgKeys * ROW, sc);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) st.st[rb].template weigh<false>(sc[rb], 0, st.c, pb[rb]);
+      st.add(s_tile, at + sub * kPgKeys * ROW, pb);
+    }
   }
+  for (; t < tiles; ++t, buffer = next_buffer(buffer)) {
+    turn(t, true);
+    const int at = buffer * M::kBuffer;
+    dropped |= s_bad[buffer] == t;
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      const int key0 = lo + t * kManyKeys + sub * kPgKeys;
+      if (key0 >= st.st[RB - 1].most && key0 >= st.st[0].most) continue;
+      pg_f16 sc[RB];
+      pg_h8 pb[RB][2];
+      st.scores(s_tile, at + sub * kPgKeys * ROW, sc);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) st.st[rb].template weigh<true>(sc[rb], key0, st.c, pb[rb]);
+      st.add(s_tile, at + sub * kPgKeys * ROW, pb);
+    }
+  }
+  __syncthreads();
   pg_append<D>(a, j, first_row, first_row + R, kManyThreads);
+  // the wavefront's rows through LDS, its own share of the tiles' room, so that they leave as whole rows
+  float *wo = (float *)s_tile + w * kPgRows * D;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const float l = st[rb].finish(src, lo, hi, dropped);
-    // the wavefront's rows through LDS, its own share of the tiles' room, so that they leave as whole rows
-    float *wo = (float *)(s_tile + w * L::kBytes);
-    st[rb].template store_partial<L::OROW>(wo + (lane & 31) * L::OROW);
+    PgRows<D> &rows = st.st[rb];
+    const float l = rows.finish(src, lo, hi, dropped);
+    const int l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int nt = 0; nt < D / 32; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)                        // (sixteen bytes to the place that keeps rows on different banks)
+        *(float4 *)(wo + l32 * D + (((8 * nt + 2 * i + h) ^ (l32 & 15)) << 2)) =
+            make_float4(rows.O[nt][4 * i], rows.O[nt][4 * i + 1], rows.O[nt][4 * i + 2], rows.O[nt][4 * i + 3]);
     pg_wave_sync();
-    const float m = st[rb].maximum(l);
+    const float m = rows.maximum(l);
 #pragma unroll
     for (int p = 0; p < kPgRows / 4; ++p) {
       const int r = 4 * p + (lane >> 4), row = first_row + (w * RB + rb) * kPgRows + r;
@@ -632,7 +724,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB
 #pragma unroll
       for (int q = 0; q < D / 64; ++q) {
         const int d = (lane & 15) * 4 + 64 * q;
-        const float4 y = *(const float4 *)(wo + r * L::OROW + d);
+        const float4 y = *(const float4 *)(wo + r * D + ((((lane & 15) + 16 * q) ^ (r & 15)) << 2));
         if (j.parts == 1) pg_write_out<D>(a, j, row, d, y, 1.f / lr);
         else *(float4 *)(a.o + ((long long)blockIdx.x * R + (w * RB + rb) * kPgRows + r) * D + d) = y;
       }
@@ -675,24 +767,32 @@ __global__ __launch_bounds__(256) void pages_merge_kernel(PagesLaunch a, int qua
 // ---------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------
-// Rows of a block: one tile where a sequence's rows fit it, else 128.
-int pages_block_rows(int tokens, int G) { return (long long)tokens * G <= kPgRows ? kPgRows : kManyWaves * kPgRows; }
-
 size_t pages_scratch_floats(int D) { return (size_t)kPagesSlots * kManyWaves * kPgRows * (D + 2); }
 
-hipError_t launch_pages(PagesLaunch a, int D, float *scratch, hipStream_t stream) {
-  const int R = pages_block_rows(a.tokens, a.G), quantum = R == kPgRows ? kFewQuantum : kManyQuantum;
-  // blocks that there can be at most; fewer than the slots: the call may be split
+template <int D, int R, typename Kernel>
+static void launch_blocks(PagesLaunch a, Kernel kernel, int threads, int quantum, float *scratch, hipStream_t stream) {
+  // Blocks that there can be at most; fewer than the slots: the call may be split.  Without counts of their own all sequences
+  // have `tokens` each: the blocks are known, and where they fill the slots none is cut.
   const long long most = (long long)a.B * (((long long)a.tokens * a.G + R - 1) / R) * a.Hkv;
-  if (most > 0x7fffffffll) return hipErrorInvalidValue;
-  // Without counts of their own all sequences have `tokens` each: the blocks are known, and where they fill the slots none is cut.
-  a.slots = scratch && (a.count || most <= kPagesSlots) ? kPagesSlots : 0;
+  const int slots = kPagesSlots * kManyWaves * kPgRows / R;
+  a.slots = scratch && (a.count || most <= slots) ? slots : 0;
   a.ml = (float2 *)scratch;
-  a.o = scratch + (size_t)kPagesSlots * R * 2;
-  const dim3 grid((unsigned)std::max<long long>(most, a.slots));
-#define CONFKV_CASE(d)                                                                                                          if (D == d) {                                                                                                                   if (R == kPgRows) {                                                                                                             hipLaunchKernelGGL(pages_few_kernel<d>, grid, dim3(kFewWaves * kWave), 0, stream, a);                                         if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<d, kPgRows>), dim3(a.slots), dim3(256), 0, stream, a, quantum);                      } else {                                                                                                                        hipLaunchKernelGGL((pages_many_kernel<d, 1>), grid, dim3(kManyThreads), 0, stream, a);                                        if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<d, kManyWaves * kPgRows>), dim3(a.slots), dim3(256), 0, stream, a, quantum);         }                                                                                                                           }
-  CONFKV_CASE(64) CONFKV_CASE(128)
-#undef CONFKV_CASE
+  a.o = scratch + (size_t)kPagesSlots * kManyWaves * kPgRows * 2;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::max<long long>(most, a.slots)), dim3(threads), 0, stream, a);
+  if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<D, R>), dim3(a.slots), dim3(256), 0, stream, a, quantum);
+}
+template <int D>
+static void launch_pages_of(const PagesLaunch &a, float *scratch, hipStream_t stream) {
+  const long long rows = (long long)a.tokens * a.G;
+  if (rows <= kPgRows)
+    launch_blocks<D, kPgRows>(a, pages_few_kernel<D>, kFewWaves * kWave, kFewQuantum, scratch, stream);
+  else
+    launch_blocks<D, kManyWaves * kPgRows>(a, pages_many_kernel<D, 1>, kManyThreads, kManyQuantum, scratch, stream);
+}
+hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream) {
+  if ((long long)a.B * a.tokens * a.G / kPgRows * a.Hkv > 0x40000000ll) return hipErrorInvalidValue;
+  if (D == 64) launch_pages_of<64>(a, scratch, stream);
+  else launch_pages_of<128>(a, scratch, stream);
   return hipGetLastError();
 }
 

@@ -157,7 +157,7 @@ void shared_plan(int rows, int Hkv, int D, int T, int cus, int forced_row_waves,
 int device_cu_count();
 hipError_t launch_shared_prefix(const SharedLaunch &a, const SharedPlan &p, int D, hipStream_t stream);
 // ---- attend_pages.hip ----
-constexpr int kPagesSlots = 256;           // (block, part) pairs of a split call at most: one workgroup per compute unit
+constexpr int kPagesSlots = 256;           // (block of 128 rows, part) pairs of a split call at most
 constexpr int kPagesLeastPart = 128;       // keys that a part has at least: calls on shorter caches are not split
 struct PagesLaunch {
   PagesView pages;
@@ -174,7 +174,7 @@ struct PagesLaunch {
   float *o;
 };
 size_t pages_scratch_floats(int D);
-hipError_t launch_pages(PagesLaunch a, int D, float *scratch, hipStream_t stream);
+hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,
 // contiguous layout).  scratch: scratch_floats floats, at least observe_scratch_floats(B * Hkv, G, T); with more the
 // work is cut into parts, observe_plan_floats(B * Hkv, G, T, first block of rows, INT8 slots, chan, scratch_floats, CUs) of them are used.
