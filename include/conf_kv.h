@@ -117,8 +117,8 @@ typedef struct conf_kv_config {
   int32_t layout;            /* conf_kv_layout: where the INT8 slots of a unit live              */
   int32_t max_shared;        /* most tokens of a shared prefix that conf_kv_attend_shared may be given (sizes the scratch
                                 buffer: up to 64 partial results per query row), up to 2^30; 0: none         */
-  int32_t max_paged;         /* most tokens of a sequence in the pages that conf_kv_attend_pages may be given (above 128: 256
-                                blocks of 128 partial results in the scratch buffer), up to 2^30; 0: none     */
+  int32_t max_paged;         /* most tokens of a sequence in the pages that conf_kv_attend_pages may be given (above 128: room
+                                for 65536 partial results in the scratch buffer), up to 2^30; 0: none     */
 } conf_kv_config;
 
 typedef enum conf_kv_layout {

@@ -28,7 +28,7 @@ struct StateLayout {
 };
 
 struct ScratchLayout {
-  size_t conf_partial, part_ml, part_o, shared_ml, shared_o, paged, spill, score, src, sel, shared, total;
+  size_t conf_partial, part_ml, part_o, paged_arrived, shared_ml, shared_o, paged, spill, score, src, sel, shared, total;
   size_t zero_bytes;     // [0, zero_bytes) holds the counters and is zeroed at create
 };
 
@@ -140,6 +140,8 @@ ScratchLayout scratch_layout(const conf_kv_config *c) {
   s.part_ml = take(UPL * kAttendMaxSplits * R * 2 * 8);
   // (the matrix-core body exchanges 128-channel partials whatever the head dimension)
   s.part_o = take(UPL * kAttendMaxSplits * R * std::max<size_t>(D, 128) * 8);
+  // parts of a paged cache's blocks that have arrived
+  s.paged_arrived = take(c->max_paged > kPagesLeastPart ? kPagesCounters * sizeof(unsigned) : 0);
   s.zero_bytes = off;
   // partial results of a shared prefix (rows of a call: at most 16 per unit)
   const size_t parts = shared_parts_most(c->max_shared);
@@ -458,6 +460,7 @@ int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const co
   a.Hkv = H;
   a.G = G;
   a.sm_scale = h->cfg.sm_scale;
+  a.arrived = (unsigned *)(h->scratch + h->kl.paged_arrived);
   CK_HIP(h, launch_pages(a, D, h->kl.paged < h->kl.spill ? (float *)(h->scratch + h->kl.paged) : nullptr, (hipStream_t)stream));
   return CONF_KV_OK;
 }

@@ -2,7 +2,7 @@
 //
 // Rows of a kv-head are (token, head of the group), token first, so that all heads of the group share the tiles.  A workgroup takes
 // a block of rows of one (sequence, kv-head) against the keys those rows see, or against a part of them where there are fewer
-// blocks than compute units; parts leave float32 partial results which a second launch merges:
+// blocks than compute units; parts leave float32 partial results which the last of them merges:
 //   ml[slot][row] = (m, l),  o[slot][row][D] = sum over the part's keys of 2^(s - m) v,   s: scores times log2(e)
 // Products are formed transposed, scores [32 keys x 32 rows] and output [D x 32 rows] (v_mfma_f32_32x32x16_f16): a lane then holds
 // values of one row only, its probabilities are the operand of the second product as they stand, and the row's statistics
@@ -30,15 +30,13 @@ __device__ __forceinline__ pg_h4 pg_read_tr(const uint8_t *p) {
 }
 __device__ __forceinline__ float pg_other_half(float v) { return __shfl_xor(v, 32, kWave); }
 // The signs of the result: which of two halfs are infinite or NaN (their magnitude, 0x7c00 or more, carries into the sign).
-__device__ __forceinline__ unsigned pg_odd_halfs(int d) { return ((unsigned)d & 0x7fff7fffu) + 0x04000400u; }
-__device__ __forceinline__ unsigned pg_odd_piece(const int4 &v) {
-  return (pg_odd_halfs(v.x) | pg_odd_halfs(v.y) | pg_odd_halfs(v.z) | pg_odd_halfs(v.w)) & 0x80008000u;
+typedef unsigned pg_u4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ pg_u4 pg_odd_halfs(pg_u4 d) { return ((d & 0x7fff7fffu) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ bool pg_odd_piece(pg_u4 v) {
+  const pg_u4 o = pg_odd_halfs(v);
+  return (o.x | o.y | o.z | o.w) != 0u;
 }
-__device__ __forceinline__ void pg_drop_odd(int4 &v) {
-  int *d = &v.x;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) d[k] &= (int)~(((pg_odd_halfs(d[k]) & 0x80008000u) >> 15) * 0xffffu);
-}
+__device__ __forceinline__ pg_u4 pg_without_odd(pg_u4 v) { return v & ~((pg_odd_halfs(v) >> 15) * 0xffffu); }
 // LDS operations of a wavefront execute in order: between lanes that exchange data only the compiler has to keep it.
 __device__ __forceinline__ void pg_wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -65,66 +63,79 @@ __device__ __forceinline__ PgSequence pg_sequence(const PagesLaunch &a, int b) {
 }
 
 struct PgJob {
-  int b, g, block, part, parts, part_keys, blocks;
+  int b, g, block, part, parts, part_keys;
   PgSequence q;
 };
+// Inclusive prefix sums over the wavefront by lane moves (an exchange through LDS takes ten times as long).
+__device__ __forceinline__ int pg_scan(int v) {
+#define CONFKV_DPP(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+  CONFKV_DPP(0x111, 0xf);                              // row_shr:1
+  CONFKV_DPP(0x112, 0xf);                              // row_shr:2
+  CONFKV_DPP(0x114, 0xf);                              // row_shr:4
+  CONFKV_DPP(0x118, 0xf);                              // row_shr:8
+  CONFKV_DPP(0x142, 0xa);                              // row_bcast:15, rows 1 and 3
+  CONFKV_DPP(0x143, 0xc);                              // row_bcast:31, rows 2 and 3
+#undef CONFKV_DPP
+  return v;
+}
+__device__ __forceinline__ int pg_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
 // Parts of equal length for all sequences, the shortest for which every (block, part) has a slot; the blocks of a
 // sequence from the last one on, whose rows see the most keys.  False: the workgroup has nothing to do.
-__device__ __forceinline__ bool pg_job(const PagesLaunch &a, int rows_per_block, int quantum, unsigned x, PgJob &j) {
+template <int R, int QUANTUM>
+__device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &j) {
   const int lane = threadIdx.x & 63;
-  j.g = x % (unsigned)a.Hkv;
-  int at = x / (unsigned)a.Hkv;
-  auto blocks_of = [&](int b, PgSequence &q) {
-    q = PgSequence{0, 0, 0};
-    if (b < a.B) q = pg_sequence(a, b);
-    return (int)(((long long)q.n * a.G + rows_per_block - 1) / rows_per_block);
-  };
-  int keys = kNoSplit;
-  PgSequence q;
+  const PgSequence mine = lane < a.B ? pg_sequence(a, lane) : PgSequence{0, 0, 0};
+  auto sequence = [&](int b0) { return b0 == 0 ? mine : b0 + lane < a.B ? pg_sequence(a, b0 + lane) : PgSequence{0, 0, 0}; };
+  // (n * G is below 2^30, lengths below 2^30 + 2^30)
+  auto blocks_of = [&](const PgSequence &q) { return (int)(((unsigned)q.n * (unsigned)a.G + (R - 1)) / R); };
+  auto length = [](const PgSequence &q) { return (unsigned)(q.c + q.n + (QUANTUM - 1)) / QUANTUM; };   // in quanta
+  unsigned part = 0;                                   // quanta of a part; 0: none is cut
   if (a.slots > 0) {
-    long long blocks = 0, work = 0;
+    const unsigned most = (unsigned)a.slots / (unsigned)a.Hkv;   // (block, part) pairs per kv-head
+    int blocks = 0;
+    float work = 0.f;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-      const int mine = blocks_of(b0 + lane, q);
-      blocks += wave_sum(mine);
-      // (in quanta, so that sixty-four of them fit: at most 2^30 / 128 keys times the blocks of a call that may split)
-      const float w = (float)mine * (float)((q.c + q.n + quantum - 1) / quantum);
-      work += (long long)wave_sum(w);
+      const PgSequence q = sequence(b0);
+      const int n = blocks_of(q);
+      blocks += pg_last(pg_scan(n));
+      work += (float)pg_last(pg_scan((int)fminf((float)n * (float)length(q), 0x1p24f)));   // (an estimate to begin with)
     }
-    if (blocks * a.Hkv <= a.slots && blocks > 0) {
-      long long k = max(1ll, (work * a.Hkv + a.slots - 1) / a.slots);      // quanta per part
+    if (blocks > 0 && (unsigned)blocks <= most) {
+      part = max(1u, (unsigned)(work / (float)most));
       for (;;) {
-        long long jobs = 0;
+        unsigned jobs = 0;
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
-          const int mine = blocks_of(b0 + lane, q);
-          const long long len = (q.c + q.n + quantum - 1) / quantum;
-          jobs += wave_sum((int)min((long long)mine * ((len + k - 1) / k), 1ll << 20));
+          const PgSequence q = sequence(b0);
+          jobs += (unsigned)pg_last(pg_scan((int)min((unsigned long long)blocks_of(q) * ((length(q) + part - 1) / part), 1ull << 24)));
         }
-        if (jobs * a.Hkv <= a.slots) break;
-        k += (k + 7) / 8;
+        if (jobs <= most) break;
+        part += (part + 15) / 16;
       }
-      keys = (int)min(k * quantum, (long long)kNoSplit);
     }
   }
-  j.part_keys = keys;
+  j.g = x % (unsigned)a.Hkv;
+  int at = x / (unsigned)a.Hkv;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int mine = blocks_of(b0 + lane, q);
-    const int parts = keys == kNoSplit ? 1 : max(1, (q.c + q.n + keys - 1) / keys);
-    const int jobs = mine * parts, end = wave_scan_incl(jobs);
+    const PgSequence q = sequence(b0);
+    const int blocks = blocks_of(q), parts = part ? (int)((length(q) + part - 1) / part) : 1;
+    const int jobs = blocks * parts, end = pg_scan(jobs);
     const unsigned long long hit = __builtin_amdgcn_ballot_w64(at < end);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       at -= __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(jobs, l);
       j.b = b0 + l;
       j.parts = __builtin_amdgcn_readlane(parts, l);
-      j.blocks = __builtin_amdgcn_readlane(mine, l);
-      j.block = j.blocks - 1 - at / j.parts;
-      j.part = at - (at / j.parts) * j.parts;
+      j.block = at / j.parts;
+      j.part = at - j.block * j.parts;
+      j.block = __builtin_amdgcn_readlane(blocks, l) - 1 - j.block;
+      j.part_keys = j.parts > 1 ? (int)(part * QUANTUM) : kNoSplit;
       j.q.n = __builtin_amdgcn_readlane(q.n, l);
       j.q.c = __builtin_amdgcn_readlane(q.c, l);
       j.q.s = __builtin_amdgcn_readlane(q.s, l);
       return true;
     }
-    at -= __builtin_amdgcn_readlane(end, 63);
+    at -= pg_last(end);
   }
   return false;
 }
@@ -164,7 +175,7 @@ struct PgSource {
     e = min(max(e, 0), n_pages - 1);
     return e * page_stride + (r0 & ((1 << lg) - 1)) * token_stride;
   }
-  __device__ __forceinline__ void load(int r0, int e, int4 &kr, int4 &vr) const {
+  __device__ __forceinline__ void load(int r0, int e, pg_u4 &kr, pg_u4 &vr) const {
     const long long o = page_offset(r0, e) + lane_off;
     const __half *kp = k + o, *vp = v + o;
     if (r0 + RWI > c) {                                // (tokens of the call among them; behind the last one its row again)
@@ -175,8 +186,8 @@ struct PgSource {
         vp = vnew + m;
       }
     }
-    kr = *(const int4 *)kp;
-    vr = *(const int4 *)vp;
+    kr = *(const pg_u4 *)kp;
+    vr = *(const pg_u4 *)vp;
   }
   __device__ __forceinline__ const __half *value_row(int t) const {
     if (t >= c) return vnew + (t - c) * new_stride;
@@ -234,38 +245,50 @@ struct PgRows {
       sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[s], sc, 0, 0, 0);
     }
   }
-  // scores of keys key0 .. key0 + 31 -> probabilities; element i: key key0 + 8 (i / 4) + 4 h + i % 4
-  // (kMask: some may be behind what a row sees)
+  // The lane's largest score of keys key0 .. key0 + 31; element i: key key0 + 8 (i / 4) + 4 h + i % 4 (kMask: some may be behind what
+  // a row sees, and leave).
   template <bool kMask>
-  __device__ __forceinline__ void weigh(pg_f16 &sc, int key0, float c, pg_h8 (&pb)[2]) {
+  __device__ __forceinline__ float peak(pg_f16 &sc, int key0) const {
     const int h = (threadIdx.x & 63) >> 5;
-    const float NEG = -INFINITY;
     if (kMask && key0 + kPgKeys > least) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + (i & 3) < lim - key0 - 4 * h ? sc[i] : NEG;
+      for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + (i & 3) < lim - key0 - 4 * h ? sc[i] : -INFINITY;
     }
     float mx = sc[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
-    // The reference only has to stay near the maximum (the merges are exact for any), so the exchange and the rescaling run
-    // where a score passes it by more than kSlack.
-    if (__builtin_amdgcn_ballot_w64(fmaf(mx, c, off) > kLift + kSlack)) {
-      const float top = fmaxf(mx, pg_other_half(mx)) * c;
-      const float now = fminf(off, kLift - top);       // (no score yet: top is -inf and off stays)
-      const float corr = off == now ? 1.f : __builtin_amdgcn_exp2f(now - off);
-      off = now;
-      l *= corr;
+    return mx;
+  }
+  // The reference only has to stay near the maximum (the merges are exact for any), so the exchange and the rescaling run
+  // where a score passes it by more than kSlack.
+  __device__ __forceinline__ bool passes(float mx, float c) const { return fmaf(mx, c, off) > kLift + kSlack; }
+  __device__ __forceinline__ void raise(float mx, float c) {
+    const float top = fmaxf(mx, pg_other_half(mx)) * c;
+    const float now = fminf(off, kLift - top);         // (no score yet: top is -inf and off stays)
+    const float corr = off == now ? 1.f : __builtin_amdgcn_exp2f(now - off);
+    off = now;
+    l *= corr;
 #pragma unroll
-      for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
-    }
+    for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
+  }
+  // scores -> probabilities
+  __device__ __forceinline__ void weights(const pg_f16 &sc, float c, pg_h8 (&pb)[2]) {
     const float at = off == INFINITY ? 0.f : off;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c, at));
-      l += p;
+      sum[i & 3] += p;
       // (fp16 operands: half a step, 2^-11 of each probability)
       pb[i / 8][i & 7] = (_Float16)p;
     }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  template <bool kMask>
+  __device__ __forceinline__ void weigh(pg_f16 &sc, int key0, float c, pg_h8 (&pb)[2]) {
+    const float mx = peak<kMask>(sc, key0);
+    if (__builtin_amdgcn_ballot_w64(passes(mx, c))) raise(mx, c);
+    weights(sc, c, pb);
   }
   template <int VROW>
   __device__ __forceinline__ void add(const uint8_t *Vt, const pg_h8 (&pb)[2]) {
@@ -320,8 +343,8 @@ struct PgRows {
 #pragma unroll 1
       for (int r0 = lo; r0 < hi; r0 += RWI) {
         const int t = min(r0 + lane / PR, hi - 1);
-        const int4 v = *(const int4 *)(src.value_row(t) + lane % PR * 8);
-        if (__builtin_amdgcn_ballot_w64(pg_odd_piece(v) != 0u) == 0ull) continue;
+        const pg_u4 v = *(const pg_u4 *)(src.value_row(t) + lane % PR * 8);
+        if (__builtin_amdgcn_ballot_w64(pg_odd_piece(v)) == 0ull) continue;
 #pragma unroll 1
         for (int key = r0; key < min(r0 + RWI, hi); ++key) {
           const __half *vr = src.value_row(key);
@@ -385,6 +408,102 @@ __device__ __forceinline__ void pg_write_out(const PagesLaunch &a, const PgJob &
   if (real) *(pg_h4 *)(pg_out_row<D>(a, j, row) + d) = pg_h4{(_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
 }
 
+// ---------------------------------------------------------------------------------------
+// The parts of a block: partial results go to scratch, and the workgroup that is last there merges them.  They go and come at
+// device scope, past the L2 of the workgroup's XCD, so that no cache is written back or emptied; a part is counted once its stores have
+// been acknowledged.  The counter goes back to zero for the next call.  (A merge in a launch of its own took 8 to 20 us.)
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ void pg_store8(float *to, float x, float y) {
+  __hip_atomic_store((unsigned long long *)to, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 pg_load8(const float *from) {
+  const unsigned long long v = __hip_atomic_load((const unsigned long long *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+template <int D, int R>
+struct PgParts {
+  static __device__ __forceinline__ long long at(int row) { return (long long)blockIdx.x * R + row; }
+  static __device__ __forceinline__ void store(const PagesLaunch &a, int row, int d, const float4 &y) {
+    float *to = a.o + at(row) * D + d;
+    pg_store8(to, y.x, y.y);
+    pg_store8(to + 2, y.z, y.w);
+  }
+  static __device__ __forceinline__ void store_sums(const PagesLaunch &a, int row, float m, float l) { pg_store8((float *)(a.ml + at(row)), m, l); }
+  // Behind the stores, all threads of the workgroup.
+  static __device__ __forceinline__ void merge(const PagesLaunch &a, const PgJob &j, int threads) {
+    __shared__ int s_last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const unsigned first = blockIdx.x - j.part * a.Hkv;  // the slot of part 0, whose counter is the block's
+    if (threadIdx.x == 0) {
+      const unsigned before = __hip_atomic_fetch_add(a.arrived + first, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      s_last = before == (unsigned)j.parts - 1u;
+      if (s_last) __hip_atomic_store(a.arrived + first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!s_last) return;
+    const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row), d = (threadIdx.x & 15) * 4, each = threads / 16;
+    const long long apart = (long long)a.Hkv * R;
+    constexpr int kSide = 2, kAhead = 4;                 // rows of a thread, parts whose words are requested together
+    for (int r0 = 0; r0 < rows; r0 += kSide * each) {
+      const float *ml[kSide], *o[kSide];
+      float M[kSide], l[kSide];
+      float4 y[kSide][D / 64];
+#pragma unroll
+      for (int i = 0; i < kSide; ++i) {
+        const long long r = (long long)first * R + min(r0 + i * each + (int)(threadIdx.x >> 4), R - 1);   // (past the last row: what nothing reads)
+        ml[i] = (const float *)(a.ml + r);
+        o[i] = a.o + r * D + d;
+        M[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) y[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      for (int p0 = 0; p0 < j.parts; p0 += kAhead) {
+        float2 s[kSide][kAhead], x[kSide][kAhead][D / 64][2];
+#pragma unroll
+        for (int i = 0; i < kSide; ++i)
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) {
+            const long long p = min(p0 + k, j.parts - 1) * apart;
+            s[i][k] = pg_load8(ml[i] + 2 * p);
+#pragma unroll
+            for (int q = 0; q < D / 64; ++q) {
+              x[i][k][q][0] = pg_load8(o[i] + p * D + 64 * q);
+              x[i][k][q][1] = pg_load8(o[i] + p * D + 64 * q + 2);
+            }
+          }
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) {
+          float now = M[i];
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) now = fmaxf(now, s[i][k].x);
+          const float f0 = pg_weight(M[i], now);
+          l[i] = f0 == 0.f ? 0.f : l[i] * f0;
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q) {
+            const float4 was = y[i][q];
+            y[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            pg_add4(y[i][q], f0, was);
+          }
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) {
+            const float f = p0 + k < j.parts ? pg_weight(s[i][k].x, now) : 0.f;
+            l[i] = f == 0.f ? l[i] : fmaf(f, s[i][k].y, l[i]);
+#pragma unroll
+            for (int q = 0; q < D / 64; ++q) pg_add4(y[i][q], f, make_float4(x[i][k][q][0].x, x[i][k][q][0].y, x[i][k][q][1].x, x[i][k][q][1].y));
+          }
+          M[i] = now;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kSide; ++i)
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + r0 + i * each + (int)(threadIdx.x >> 4), d + 64 * q, y[i][q], 1.f / l[i]);
+    }
+  }
+};
+
 // The new tokens whose first row lies in rows [lo, hi) of the sequence go to their pages (an entry that is no page: nowhere).
 template <int D>
 __device__ __forceinline__ void pg_append(const PagesLaunch &a, const PgJob &j, int lo, int hi, int threads) {
@@ -412,12 +531,13 @@ struct PgTile {
 };
 
 // ---------------------------------------------------------------------------------------
-// Up to 32 rows of a (sequence, kv-head), single tokens above all: bound by the bytes of K and V.  Eight wavefronts take the
+// Up to 32 rows of a (sequence, kv-head), single tokens above all: bound by the bytes of K and V.  Four wavefronts take the
 // part's tiles of 32 keys in turn; a wavefront waits for nobody before the merge: it loads and multiplies tiles of its own, the
 // next one in flight in registers while this one is used.
 // ---------------------------------------------------------------------------------------
-constexpr int kManyQuantum = kPagesLeastPart;
-constexpr int kFewWaves = 8, kFewQuantum = kFewWaves * kPgKeys;
+constexpr int kManyQuantum = 256;
+constexpr int kFewWaves = 4, kFewQuantum = kFewWaves * kPgKeys;
+static_assert(kFewQuantum == kPagesLeastPart);
 
 template <int D>
 __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void pages_few_kernel(PagesLaunch a) {
@@ -427,16 +547,16 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   __shared__ float s_m[kFewWaves][kPgRows], s_l[kFewWaves][kPgRows];
   static_assert(kPgRows * L::OROW * 4 <= L::kBytes, "a wavefront's partial fits its tile");
   PgJob j;
-  if (!pg_job(a, kPgRows, kFewQuantum, blockIdx.x, j)) return;
+  if (!pg_job<kPgRows, kFewQuantum>(a, blockIdx.x, j)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   PgSource<D> src;
   src.init(a, j);
   const int first_row = j.block * kPgRows;
-  const int lo = j.part_keys == kNoSplit ? 0 : j.part * j.part_keys;
+  const int lo = j.parts > 1 ? j.part * j.part_keys : 0;
   const int hi = (int)min((long long)lo + j.part_keys, (long long)(j.q.c + j.q.n));
   PgRows<D> st;
-  struct Turn { int4 k[NP], v[NP]; } x;
+  struct Turn { pg_u4 k[NP], v[NP]; } x;
   auto load = [&](int base, int ent) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) src.load(base + RWI * i, __builtin_amdgcn_readlane(ent, RWI * i), x.k[i], x.v[i]);
@@ -457,20 +577,17 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     // Keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN value: where there
     // are such rows these values leave the tile here and reach the rows that do see them at the end.
     if (key0 + kPgKeys > st.least) {
-      unsigned odd = 0u;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) odd |= pg_odd_piece(x.v[i]);
-      if (__builtin_expect(odd != 0u, 0)) {
-        dropped = true;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) pg_drop_odd(x.v[i]);
+      for (int i = 0; i < NP; ++i) {
+        dropped |= pg_odd_piece(x.v[i]);
+        x.v[i] = pg_without_odd(x.v[i]);
       }
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int row = RWI * i + lane / PR;
-      *(int4 *)(Kt + row * L::KROW + lane % PR * 16) = x.k[i];
-      *(int4 *)(Vt + row * L::VROW + lane % PR * 16) = x.v[i];
+      *(pg_u4 *)(Kt + row * L::KROW + lane % PR * 16) = x.k[i];
+      *(pg_u4 *)(Vt + row * L::VROW + lane % PR * 16) = x.v[i];
     }
     pg_wave_sync();
     if (key0 + kFewQuantum < end) {
@@ -494,7 +611,9 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   pg_append<D>(a, j, first_row, first_row + kPgRows, kFewWaves * kWave);
   __syncthreads();
   // sixteen threads per row merge the wavefronts' partials
-  const int row = tid >> 4;
+  const int rows = min(kPgRows, j.q.n * a.G - first_row);
+  for (int r0 = 0; r0 < rows; r0 += kFewWaves * 4) {
+  const int row = r0 + (tid >> 4);
   float m[kFewWaves], M = -INFINITY, l = 0.f;
 #pragma unroll
   for (int k = 0; k < kFewWaves; ++k) {
@@ -512,13 +631,12 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
-    if (j.parts == 1) {
-      pg_write_out<D>(a, j, first_row + row, d, y, 1.f / l);
-    } else {
-      *(float4 *)(a.o + ((long long)blockIdx.x * kPgRows + row) * D + d) = y;
-    }
+    if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / l);
+    else if (row < rows) PgParts<D, kPgRows>::store(a, row, d, y);
   }
-  if (j.parts > 1 && (tid & 15) == 0) a.ml[(long long)blockIdx.x * kPgRows + row] = make_float2(M, l);
+  if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D, kPgRows>::store_sums(a, row, M, l);
+  }
+  if (j.parts > 1) PgParts<D, kPgRows>::merge(a, j, kFewWaves * kWave);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -528,7 +646,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 // pieces of a row are permuted instead: piece p of row r lies at slot p ^ f(r), with an f that puts what the reads below take
 // together on different banks -- eight lanes' pieces of K at one place of their rows, the pieces of four neighbouring V rows.
 // ---------------------------------------------------------------------------------------
-constexpr int kManyWaves = 4, kManyKeys = 64, kManyThreads = kManyWaves * kWave;
+constexpr int kManyWaves = 8, kManyKeys = 64, kManyBuffers = 3, kManyThreads = kManyWaves * kWave, kManyRows = kManyWaves * kPgRows;
 
 template <int D>
 __device__ __forceinline__ constexpr int pg_swizzle(int r) {
@@ -538,6 +656,12 @@ __device__ __forceinline__ constexpr int pg_swizzle(int r) {
 __device__ __forceinline__ void pg_load_lds(const void *from, unsigned to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
+// The same from `from`, alike in all lanes, plus the lane's offset in bytes.
+__device__ __forceinline__ void pg_load_lds(const void *from, unsigned offset, unsigned to) {
+  const unsigned long long p = (unsigned long long)from;
+  const unsigned long long at = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)p);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(at) : "memory");
+}
 __device__ __forceinline__ unsigned pg_lds_at(const void *p) {
   return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
 }
@@ -545,66 +669,57 @@ __device__ __forceinline__ unsigned pg_lds_at(const void *p) {
 __device__ __forceinline__ void pg_arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void pg_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
-template <int D, int RB>
+template <int D>
 struct PgMany {
   static constexpr int PR = D / 8, RWI = kWave / PR, RPP = kManyThreads / PR, NP = kManyKeys / RPP, ROW = 2 * D;
-  static constexpr int R = kManyWaves * RB * kPgRows;
-  static constexpr int kPlane = kManyKeys * ROW, kBuffer = 2 * kPlane, kBuffers = RB == 1 ? 2 : 3;
+  static constexpr int kPlane = kManyKeys * ROW, kBuffer = 2 * kPlane, kSub = kPgKeys * ROW;
 
-  PgRows<D> st[RB];
+  PgRows<D> rows;
   float c;
   int k_off, v_off;                                    // the lane's places in a tile: K fragment 0, V fragment 0
 
   __device__ __forceinline__ void init(const PagesLaunch &a, const PgJob &j, int first_row) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, t16 = lane & 15, c2 = (lane >> 4) & 1;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) st[rb].init(a, j, first_row + (w * RB + rb) * kPgRows);
+    rows.init(a, j, first_row + w * kPgRows);
     c = a.sm_scale * 1.44269504088896341f;
     k_off = l32 * ROW + ((h ^ pg_swizzle<D>(l32)) << 4);
     const int vr = 4 * h + (t16 >> 2);
     v_off = kPlane + vr * ROW + (((2 * c2 + ((t16 & 3) >> 1)) ^ pg_swizzle<D>(vr)) << 4) + 8 * (t16 & 1);
   }
   // scores of the 32 keys at byte offset `at`
-  __device__ __forceinline__ void scores(const uint8_t *lds, int at, pg_f16 (&sc)[RB]) const {
+  __device__ __forceinline__ void scores(const uint8_t *lds, int at, pg_f16 &sc) const {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[rb][i] = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      const pg_h8 kf = *(const pg_h8 *)(lds + at + (k_off ^ (s << 5)));
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, st[rb].qf[s], sc[rb], 0, 0, 0);
-    }
+    for (int s = 0; s < D / 16; ++s)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const pg_h8 *)(lds + at + (k_off ^ (s << 5))), rows.qf[s], sc, 0, 0, 0);
   }
-  __device__ __forceinline__ void add(const uint8_t *lds, int at, const pg_h8 (&pb)[RB][2]) {
+  __device__ __forceinline__ void add(const uint8_t *lds, int at, const pg_h8 (&pb)[2]) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int nt = 0; nt < D / 32; ++nt) {
         const uint8_t *vp = lds + at + 16 * s * ROW;
         const pg_h4 v0 = pg_read_tr(vp + (v_off ^ (nt << 6))), v1 = pg_read_tr(vp + 8 * ROW + (v_off ^ (nt << 6) ^ 32));
-        const pg_h8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) st[rb].O[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pb[rb][s], st[rb].O[nt], 0, 0, 0);
+        rows.O[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pb[s], rows.O[nt], 0, 0, 0);
       }
   }
 };
 
-template <int D, int RB>
-__global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB == 1 ? 2 : 1, RB == 1 ? 2 : 1))) void pages_many_kernel(PagesLaunch a) {
-  using M = PgMany<D, RB>;
-  constexpr int PR = M::PR, RWI = M::RWI, RPP = M::RPP, NP = M::NP, R = M::R, ROW = M::ROW;
-  __shared__ __align__(16) uint8_t s_tile[M::kBuffers * M::kBuffer];
-  __shared__ int s_bad[M::kBuffers];
-  static_assert(kManyWaves * kPgRows * D * 4 <= sizeof(s_tile), "the wavefronts' rows fit the tiles' room");
+template <int D>
+__global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) void pages_many_kernel(PagesLaunch a) {
+  using M = PgMany<D>;
+  constexpr int PR = M::PR, RWI = M::RWI, RPP = M::RPP, NP = M::NP, R = kManyRows, ROW = M::ROW;
+  constexpr int kRoom = std::max(kManyBuffers * M::kBuffer, kManyWaves * kPgRows * 256);   // the tiles, later the rows
+  __shared__ __align__(16) uint8_t s_tile[kRoom];
+  __shared__ int s_bad[kManyBuffers];
   PgJob j;
-  if (!pg_job(a, R, kManyQuantum, blockIdx.x, j)) return;
+  if (!pg_job<R, kManyQuantum>(a, blockIdx.x, j)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   PgSource<D> src;
   src.init(a, j);
   const int first_row = j.block * R, last_row = min(first_row + R, j.q.n * a.G) - 1;
-  const int lo = j.part_keys == kNoSplit ? 0 : j.part * j.part_keys;
+  const int lo = j.parts > 1 ? j.part * j.part_keys : 0;
   const int seen = j.q.c + last_row / a.G + 1;           // keys that the block's last row sees
   const int hi = (int)min((long long)lo + j.part_keys, (long long)seen);
   const int all_least = j.q.c + first_row / a.G + 1;     // and its first one
@@ -613,35 +728,52 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB
   // The lane's row and piece of a wavefront's load; f does not depend on which of a tile's loads it is.
   const int lrow = RWI * w + lane / PR, lpiece = (lane % PR) ^ pg_swizzle<D>(lrow);
   const long long lane_off = (lane / PR) * src.token_stride + lpiece * 8;
+  const unsigned page_lane = (unsigned)(2 * lane_off), new_lane = (unsigned)(2 * ((lane / PR) * src.new_stride + lpiece * 8));
+  const bool near = src.token_stride < 1 << 26;          // (a wavefront's rows of a page less than 2^32 bytes apart)
   const unsigned lds0 = pg_lds_at(s_tile);
   int ent = src.entry(lo + lane);
   auto issue = [&](int t, int buffer) {                  // (every tile's entries were requested with the tile before)
     if (t >= tiles) return;
     const int base = lo + t * kManyKeys;
     const unsigned to = lds0 + buffer * M::kBuffer + RWI * w * ROW;
+    if (base >= src.c && base + kManyKeys <= src.n) {    // nothing but tokens of the call
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = RPP * i + RWI * w;
-      const long long o = src.page_offset(base + r, __builtin_amdgcn_readlane(ent, r)) + lane_off;
-      const __half *kp = src.k + o, *vp = src.v + o;
-      if (base + r + RWI > src.c) {                      // tokens of the call among them
-        const int token = min(base + RPP * i + lrow, src.n - 1);
-        if (token >= src.c) {
-          const long long m = (token - src.c) * src.new_stride + lpiece * 8;
+      for (int i = 0; i < NP; ++i) {
+        const long long m = (base + RPP * i + RWI * w - src.c) * src.new_stride;
+        pg_load_lds(src.knew + m, new_lane, to + RPP * i * ROW);
+        pg_load_lds(src.vnew + m, new_lane, to + M::kPlane + RPP * i * ROW);
+      }
+    } else if (base + kManyKeys <= src.c && near) {      // nothing but tokens in pages
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int r = RPP * i + RWI * w;
+        const long long o = src.page_offset(base + r, __builtin_amdgcn_readlane(ent, r));
+        pg_load_lds(src.k + o, page_lane, to + RPP * i * ROW);
+        pg_load_lds(src.v + o, page_lane, to + M::kPlane + RPP * i * ROW);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < NP; ++i) {
+        const int r = RPP * i + RWI * w, token = min(base + RPP * i + lrow, src.n - 1);
+        const long long o = src.page_offset(base + r, __builtin_amdgcn_readlane(ent, r)) + lane_off;
+        const bool fresh = base + RPP * i + lrow >= src.c;
+        const long long m = (token - src.c) * src.new_stride + lpiece * 8;
+        const __half *kp = src.k + o, *vp = src.v + o;
+        if (fresh) {
           kp = src.knew + m;
           vp = src.vnew + m;
         }
+        pg_load_lds(kp, to + RPP * i * ROW);
+        pg_load_lds(vp, to + M::kPlane + RPP * i * ROW);
       }
-      pg_load_lds(kp, to + RPP * i * ROW);
-      pg_load_lds(vp, to + M::kPlane + RPP * i * ROW);
     }
     if (t + 1 < tiles) ent = src.entry(base + kManyKeys + lane);
   };
-  if (tid < M::kBuffers) s_bad[tid] = -1;
+  if (tid < kManyBuffers) s_bad[tid] = -1;
   issue(0, 0);
   M st;
   st.init(a, j, first_row);
-  if (M::kBuffers > 2) issue(1, 1);
+  issue(1, 1);
   __syncthreads();
   bool dropped = false;
   // Values of keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN one: where
@@ -650,17 +782,16 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB
   auto scrub = [&](int t, int buffer) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      int4 *p = (int4 *)(s_tile + buffer * M::kBuffer + M::kPlane + (RPP * i + RWI * w) * ROW + lane * 16);
-      int4 v = *p;
-      if (__builtin_expect(pg_odd_piece(v) != 0u, 0)) {
+      pg_u4 *p = (pg_u4 *)(s_tile + buffer * M::kBuffer + M::kPlane + (RPP * i + RWI * w) * ROW + lane * 16);
+      const pg_u4 v = *p;
+      if (__builtin_expect(pg_odd_piece(v), 0)) {
         s_bad[buffer] = t;
-        pg_drop_odd(v);
-        *p = v;
+        *p = pg_without_odd(v);
       }
     }
   };
   int buffer = 0;
-  auto next_buffer = [&](int b) { return b + 1 == M::kBuffers ? 0 : b + 1; };
+  auto next_buffer = [&](int b) { return b + 1 == kManyBuffers ? 0 : b + 1; };
   auto turn = [&](int t, bool tail) {                    // tile t is there, and the next one but kBuffers - 2 is requested
     pg_arrive();
     if (tail) {
@@ -668,126 +799,105 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(RB
       pg_arrive();
     }
     pg_barrier();
-    issue(t + M::kBuffers - 1, buffer == 0 ? M::kBuffers - 1 : buffer - 1);
+    issue(t + kManyBuffers - 1, buffer == 0 ? kManyBuffers - 1 : buffer - 1);
   };
   int t = 0;
+  // Keys that all rows see.  The scores of the next 32 keys are formed while the exponentials of these are, their maximum while
+  // these meet the values: matrix products beside vector arithmetic in either half of a step.
+  pg_f16 sc[2];
+  float mx = 0.f;
+  auto step = [&](int at, int next, const pg_f16 &now, pg_f16 &then) {
+    pg_h8 pb[2];
+    if (__builtin_amdgcn_ballot_w64(st.rows.passes(mx, st.c))) st.rows.raise(mx, st.c);
+    __builtin_amdgcn_sched_barrier(0);
+    st.scores(s_tile, next, then);
+    st.rows.weights(now, st.c, pb);
+    __builtin_amdgcn_sched_barrier(0);
+    st.add(s_tile, at, pb);
+    mx = st.rows.template peak<false>(then, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
   for (; t < full; ++t, buffer = next_buffer(buffer)) {
     turn(t, false);
     const int at = buffer * M::kBuffer;
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      pg_f16 sc[RB];
-      pg_h8 pb[RB][2];
-      st.scores(s_tile, at + sub * kPgKeys * ROW, sc);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) st.st[rb].template weigh<false>(sc[rb], 0, st.c, pb[rb]);
-      st.add(s_tile, at + sub * kPgKeys * ROW, pb);
+    if (t == 0) {
+      st.scores(s_tile, at, sc[0]);
+      mx = st.rows.template peak<false>(sc[0], 0);
     }
+    step(at, at + M::kSub, sc[0], sc[1]);
+    // (behind the last of them: scores that are not used, of the next tile or of whatever lies there)
+    step(at + M::kSub, next_buffer(buffer) * M::kBuffer, sc[1], sc[0]);
   }
   for (; t < tiles; ++t, buffer = next_buffer(buffer)) {
     turn(t, true);
-    const int at = buffer * M::kBuffer;
     dropped |= s_bad[buffer] == t;
 #pragma unroll 1
     for (int sub = 0; sub < 2; ++sub) {
-      const int key0 = lo + t * kManyKeys + sub * kPgKeys;
-      if (key0 >= st.st[RB - 1].most && key0 >= st.st[0].most) continue;
-      pg_f16 sc[RB];
-      pg_h8 pb[RB][2];
-      st.scores(s_tile, at + sub * kPgKeys * ROW, sc);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) st.st[rb].template weigh<true>(sc[rb], key0, st.c, pb[rb]);
-      st.add(s_tile, at + sub * kPgKeys * ROW, pb);
+      const int key0 = lo + t * kManyKeys + sub * kPgKeys, at = buffer * M::kBuffer + sub * M::kSub;
+      if (key0 >= st.rows.most) break;
+      pg_h8 pb[2];
+      st.scores(s_tile, at, sc[0]);
+      st.rows.template weigh<true>(sc[0], key0, st.c, pb);
+      st.add(s_tile, at, pb);
     }
   }
   __syncthreads();
   pg_append<D>(a, j, first_row, first_row + R, kManyThreads);
-  // the wavefront's rows through LDS, its own share of the tiles' room, so that they leave as whole rows
-  float *wo = (float *)s_tile + w * kPgRows * D;
+  // the wavefront's rows through LDS, 64 channels at a time in its own share of the tiles' room, so that they leave as whole lines
+  float *wo = (float *)s_tile + w * kPgRows * 64;
+  const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l);
+  const int l32 = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    PgRows<D> &rows = st.st[rb];
-    const float l = rows.finish(src, lo, hi, dropped);
-    const int l32 = lane & 31, h = lane >> 5;
+  for (int q = 0; q < D / 64; ++q) {
 #pragma unroll
-    for (int nt = 0; nt < D / 32; ++nt)
+    for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)                        // (sixteen bytes to the place that keeps rows on different banks)
-        *(float4 *)(wo + l32 * D + (((8 * nt + 2 * i + h) ^ (l32 & 15)) << 2)) =
-            make_float4(rows.O[nt][4 * i], rows.O[nt][4 * i + 1], rows.O[nt][4 * i + 2], rows.O[nt][4 * i + 3]);
+      for (int i = 0; i < 4; ++i) {                      // (sixteen bytes to the place that keeps rows on different banks)
+        const pg_f16 &o = st.rows.O[2 * q + nt];
+        *(float4 *)(wo + l32 * 64 + (((8 * nt + 2 * i + h) ^ (l32 & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      }
     pg_wave_sync();
-    const float m = rows.maximum(l);
 #pragma unroll
     for (int p = 0; p < kPgRows / 4; ++p) {
-      const int r = 4 * p + (lane >> 4), row = first_row + (w * RB + rb) * kPgRows + r;
+      const int r = 4 * p + (lane >> 4), row = w * kPgRows + r, d = (lane & 15) * 4 + 64 * q;
       const float lr = __shfl(l, r, kWave);
-#pragma unroll
-      for (int q = 0; q < D / 64; ++q) {
-        const int d = (lane & 15) * 4 + 64 * q;
-        const float4 y = *(const float4 *)(wo + r * D + ((((lane & 15) + 16 * q) ^ (r & 15)) << 2));
-        if (j.parts == 1) pg_write_out<D>(a, j, row, d, y, 1.f / lr);
-        else *(float4 *)(a.o + ((long long)blockIdx.x * R + (w * RB + rb) * kPgRows + r) * D + d) = y;
-      }
+      const float4 y = *(const float4 *)(wo + r * 64 + (((lane & 15) ^ (r & 15)) << 2));
+      if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / lr);
+      else if (first_row + row <= last_row) PgParts<D, R>::store(a, row, d, y);
     }
-    if (j.parts > 1 && lane < kPgRows) a.ml[(long long)blockIdx.x * R + (w * RB + rb) * kPgRows + lane] = make_float2(m, l);
     pg_wave_sync();
   }
-}
-
-// ---------------------------------------------------------------------------------------
-// The parts' partial results of a block of R rows, merged: sixteen threads per row.
-// ---------------------------------------------------------------------------------------
-template <int D, int R>
-__global__ __launch_bounds__(256) void pages_merge_kernel(PagesLaunch a, int quantum) {
-  PgJob j;
-  if (!pg_job(a, R, quantum, blockIdx.x, j) || j.parts == 1 || j.part != 0) return;
-  const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row);
-  for (int r0 = 0; r0 < rows; r0 += 16) {
-    const int r = r0 + (threadIdx.x >> 4);               // (past the last row: partials that nothing reads)
-    const float2 *ml = a.ml + (long long)blockIdx.x * R + r;
-    const float *o = a.o + ((long long)blockIdx.x * R + r) * D;
-    const long long apart = (long long)a.Hkv * R;
-    float M = -INFINITY, l = 0.f;
-    for (int p = 0; p < j.parts; ++p) M = fmaxf(M, ml[p * apart].x);
-    float4 y[D / 64];
-#pragma unroll
-    for (int q = 0; q < D / 64; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p = 0; p < j.parts; ++p) {
-      const float2 s = ml[p * apart];
-      const float f = pg_weight(s.x, M);
-      l = f == 0.f ? l : fmaf(f, s.y, l);
-#pragma unroll
-      for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f, *(const float4 *)(o + p * apart * D + (threadIdx.x & 15) * 4 + 64 * q));
-    }
-#pragma unroll
-    for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + r, (threadIdx.x & 15) * 4 + 64 * q, y[q], 1.f / l);
+  if (j.parts > 1) {
+    if (lane < kPgRows && first_row + w * kPgRows + lane <= last_row) PgParts<D, R>::store_sums(a, w * kPgRows + lane, m, l);
+    PgParts<D, R>::merge(a, j, kManyThreads);
   }
 }
 
 // ---------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------
-size_t pages_scratch_floats(int D) { return (size_t)kPagesSlots * kManyWaves * kPgRows * (D + 2); }
+// Slots of a split call, by the rows of a block: a workgroup of many rows per compute unit; of few rows, whose sequences may be of any
+// length, some more, so that no part is much longer than the others.
+constexpr int kManySlots = 256, kFewSlots = kPagesCounters;
+constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
+size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
 
-template <int D, int R, typename Kernel>
-static void launch_blocks(PagesLaunch a, Kernel kernel, int threads, int quantum, float *scratch, hipStream_t stream) {
+template <int R, typename Kernel>
+static void launch_blocks(PagesLaunch a, Kernel kernel, int threads, int slots, float *scratch, hipStream_t stream) {
   // Blocks that there can be at most; fewer than the slots: the call may be split.  Without counts of their own all sequences
   // have `tokens` each: the blocks are known, and where they fill the slots none is cut.
   const long long most = (long long)a.B * (((long long)a.tokens * a.G + R - 1) / R) * a.Hkv;
-  const int slots = kPagesSlots * kManyWaves * kPgRows / R;
   a.slots = scratch && (a.count || most <= slots) ? slots : 0;
   a.ml = (float2 *)scratch;
-  a.o = scratch + (size_t)kPagesSlots * kManyWaves * kPgRows * 2;
+  a.o = scratch + kSlotRows * 2;
   hipLaunchKernelGGL(kernel, dim3((unsigned)std::max<long long>(most, a.slots)), dim3(threads), 0, stream, a);
-  if (a.slots) hipLaunchKernelGGL((pages_merge_kernel<D, R>), dim3(a.slots), dim3(256), 0, stream, a, quantum);
 }
 template <int D>
 static void launch_pages_of(const PagesLaunch &a, float *scratch, hipStream_t stream) {
-  const long long rows = (long long)a.tokens * a.G;
-  if (rows <= kPgRows)
-    launch_blocks<D, kPgRows>(a, pages_few_kernel<D>, kFewWaves * kWave, kFewQuantum, scratch, stream);
+  if ((long long)a.tokens * a.G <= kPgRows)
+    launch_blocks<kPgRows>(a, pages_few_kernel<D>, kFewWaves * kWave, kFewSlots, scratch, stream);
   else
-    launch_blocks<D, kManyWaves * kPgRows>(a, pages_many_kernel<D, 1>, kManyThreads, kManyQuantum, scratch, stream);
+    launch_blocks<kManyRows>(a, pages_many_kernel<D>, kManyThreads, kManySlots, scratch, stream);
 }
 hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream) {
   if ((long long)a.B * a.tokens * a.G / kPgRows * a.Hkv > 0x40000000ll) return hipErrorInvalidValue;

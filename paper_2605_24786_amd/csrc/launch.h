@@ -157,7 +157,6 @@ void shared_plan(int rows, int Hkv, int D, int T, int cus, int forced_row_waves,
 int device_cu_count();
 hipError_t launch_shared_prefix(const SharedLaunch &a, const SharedPlan &p, int D, hipStream_t stream);
 // ---- attend_pages.hip ----
-constexpr int kPagesSlots = 256;           // (block of 128 rows, part) pairs of a split call at most
 constexpr int kPagesLeastPart = 128;       // keys that a part has at least: calls on shorter caches are not split
 struct PagesLaunch {
   PagesView pages;
@@ -169,10 +168,12 @@ struct PagesLaunch {
   long long lambda_stride;
   int B, Hkv, G;
   float sm_scale;
-  int slots;                               // filled in by the launcher, as ml and o
+  int slots;                               // (block, part) pairs of a split call at most; filled in by the launcher, as ml and o
   float2 *ml;
   float *o;
+  unsigned *arrived;                       // [kPagesCounters], zero between calls: parts of a block that have left their results
 };
+constexpr int kPagesCounters = 1024;
 size_t pages_scratch_floats(int D);
 hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,
