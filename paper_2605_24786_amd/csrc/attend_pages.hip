@@ -66,6 +66,16 @@ struct PgJob {
   int b, g, block, part, parts, part_keys;
   PgSequence q;
 };
+// The least quanta that a part has.  Few rows: the workgroup that merges the parts, alone, reads as many bytes for every row of every
+// part as for a key, so that with parts shorter than the square root of keys * rows the merge would take longer than a part.
+// Many rows: 512 keys take as long (18 us) as the merge's launch twice.
+constexpr int kManyLeastPart = 512;
+template <int R, int QUANTUM>
+__device__ __forceinline__ unsigned pg_least_part(const PagesLaunch &a, unsigned longest) {
+  if constexpr (R != kPgRows) return kManyLeastPart / QUANTUM;
+  const float rows = (float)min((long long)a.tokens * a.G, (long long)R);
+  return max(1u, (unsigned)(__builtin_sqrtf((float)longest * QUANTUM * rows) * (1.f / QUANTUM)));
+}
 // Inclusive prefix sums over the wavefront by lane moves (an exchange through LDS takes ten times as long).
 __device__ __forceinline__ int pg_scan(int v) {
 #define CONFKV_DPP(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
@@ -82,6 +92,7 @@ __device__ __forceinline__ int pg_last(int v) { return __builtin_amdgcn_readlane
 
 // Parts of equal length for all sequences, the shortest for which every (block, part) has a slot; the blocks of a
 // sequence from the last one on, whose rows see the most keys.  False: the workgroup has nothing to do.
+// (R rows a block; parts in whole quanta of keys, and no shorter than is worth their merge, see pg_least_part.)
 template <int R, int QUANTUM>
 __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &j) {
   const int lane = threadIdx.x & 63;
@@ -94,15 +105,17 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
   if (a.slots > 0) {
     const unsigned most = (unsigned)a.slots / (unsigned)a.Hkv;   // (block, part) pairs per kv-head
     int blocks = 0;
+    unsigned longest = 0;
     float work = 0.f;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
       const PgSequence q = sequence(b0);
       const int n = blocks_of(q);
       blocks += pg_last(pg_scan(n));
       work += (float)pg_last(pg_scan((int)fminf((float)n * (float)length(q), 0x1p24f)));   // (an estimate to begin with)
+      longest = max(longest, (unsigned)wave_max((int)length(q)));
     }
     if (blocks > 0 && (unsigned)blocks <= most) {
-      part = max(1u, (unsigned)(work / (float)most));
+      part = max(pg_least_part<R, QUANTUM>(a, longest), (unsigned)(work / (float)most));
       for (;;) {
         unsigned jobs = 0;
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
@@ -119,8 +132,20 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const PgSequence q = sequence(b0);
     const int blocks = blocks_of(q), parts = part ? (int)((length(q) + part - 1) / part) : 1;
-    const int jobs = blocks * parts, end = pg_scan(jobs);
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(at < end);
+    const int jobs = blocks * parts;
+    int end = pg_scan(jobs);
+    const int all = pg_last(end);
+    if (R != kPgRows && a.B > 1 && a.B <= kWave) {
+      // long sequences first: the workgroups that come last shall have little to do (16 sequences of 0 to 700 tokens behind up
+      // to 5000: 416 -> 330 us)
+      const int len = q.c + q.n;
+      end = jobs;
+      for (int i = 0; i < a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        end += other > len || (other == len && i < lane) ? __builtin_amdgcn_readlane(jobs, i) : 0;
+      }
+    }
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(at < end && at >= end - jobs);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       at -= __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(jobs, l);
@@ -135,7 +160,7 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
       j.q.s = __builtin_amdgcn_readlane(q.s, l);
       return true;
     }
-    at -= pg_last(end);
+    at -= all;
   }
   return false;
 }
@@ -384,11 +409,11 @@ __device__ __forceinline__ float pg_weight(float m, float M) {
 }
 // y += f x (f zero, of a result without keys: whatever x holds)
 __device__ __forceinline__ void pg_add4(float4 &y, float f, const float4 &x) {
-  if (f == 0.f) return;
-  y.x = fmaf(f, x.x, y.x);
-  y.y = fmaf(f, x.y, y.y);
-  y.z = fmaf(f, x.z, y.z);
-  y.w = fmaf(f, x.w, y.w);
+  const bool some = f != 0.f;
+  y.x = some ? fmaf(f, x.x, y.x) : y.x;
+  y.y = some ? fmaf(f, x.y, y.y) : y.y;
+  y.z = some ? fmaf(f, x.z, y.z) : y.z;
+  y.w = some ? fmaf(f, x.w, y.w) : y.w;
 }
 // Channels d .. d + 3 of row `row`, sums y over its normaliser; sixteen neighbouring lanes hold a row, the next sixteen the next one.
 // Heads that are subtracted in pairs: the even row takes the odd one's from there.  (All lanes call it.)
@@ -409,9 +434,9 @@ __device__ __forceinline__ void pg_write_out(const PagesLaunch &a, const PgJob &
 }
 
 // ---------------------------------------------------------------------------------------
-// The parts of a block: partial results go to scratch, and the workgroup that is last there merges them.  They go and come at
-// device scope, past the L2 of the workgroup's XCD, so that no cache is written back or emptied; a part is counted once its stores have
-// been acknowledged.  The counter goes back to zero for the next call.  (A merge in a launch of its own took 8 to 20 us.)
+// The parts of a block of few rows: partial results go to scratch, and the workgroup that is last there merges them.  They go and
+// come at device scope, past the L2 of the workgroup's XCD, so that no cache is written back or emptied; a part is counted once its
+// stores have been acknowledged.  The counter goes back to zero for the next call.  (A merge in a launch of its own took 6 to 20 us.)
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ void pg_store8(float *to, float x, float y) {
   __hip_atomic_store((unsigned long long *)to, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -420,8 +445,9 @@ __device__ __forceinline__ float2 pg_load8(const float *from) {
   const unsigned long long v = __hip_atomic_load((const unsigned long long *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
-template <int D, int R>
+template <int D>
 struct PgParts {
+  static constexpr int R = kPgRows;
   static __device__ __forceinline__ long long at(int row) { return (long long)blockIdx.x * R + row; }
   static __device__ __forceinline__ void store(const PagesLaunch &a, int row, int d, const float4 &y) {
     float *to = a.o + at(row) * D + d;
@@ -535,7 +561,7 @@ struct PgTile {
 // part's tiles of 32 keys in turn; a wavefront waits for nobody before the merge: it loads and multiplies tiles of its own, the
 // next one in flight in registers while this one is used.
 // ---------------------------------------------------------------------------------------
-constexpr int kManyQuantum = 256;
+constexpr int kManyQuantum = 64;
 constexpr int kFewWaves = 4, kFewQuantum = kFewWaves * kPgKeys;
 static_assert(kFewQuantum == kPagesLeastPart);
 
@@ -632,11 +658,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 #pragma unroll
     for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
     if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / l);
-    else if (row < rows) PgParts<D, kPgRows>::store(a, row, d, y);
+    else if (row < rows) PgParts<D>::store(a, row, d, y);
   }
-  if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D, kPgRows>::store_sums(a, row, M, l);
+  if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D>::store_sums(a, row, M, l);
   }
-  if (j.parts > 1) PgParts<D, kPgRows>::merge(a, j, kFewWaves * kWave);
+  if (j.parts > 1) PgParts<D>::merge(a, j, kFewWaves * kWave);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -863,13 +889,45 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
       const float lr = __shfl(l, r, kWave);
       const float4 y = *(const float4 *)(wo + r * 64 + (((lane & 15) ^ (r & 15)) << 2));
       if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / lr);
-      else if (first_row + row <= last_row) PgParts<D, R>::store(a, row, d, y);
+      else if (first_row + row <= last_row) *(float4 *)(a.o + ((long long)blockIdx.x * R + row) * D + d) = y;
     }
     pg_wave_sync();
   }
-  if (j.parts > 1) {
-    if (lane < kPgRows && first_row + w * kPgRows + lane <= last_row) PgParts<D, R>::store_sums(a, w * kPgRows + lane, m, l);
-    PgParts<D, R>::merge(a, j, kManyThreads);
+  if (j.parts > 1 && lane < kPgRows) a.ml[(long long)blockIdx.x * R + w * kPgRows + lane] = make_float2(m, l);
+}
+
+// Many rows: their parts' partial results are merged in a launch of its own, by as many workgroups as there are parts: alone, a
+// compute unit would read the 540 KB of four parts in 28 us.
+template <int D>
+__global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a) {
+  constexpr int R = kManyRows, kEach = kManyThreads / 16;   // sixteen threads per row
+  PgJob j;
+  if (!pg_job<R, kManyQuantum>(a, blockIdx.x, j) || j.parts == 1) return;
+  const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row), d = (threadIdx.x & 15) * 4;
+  const int share = ((rows + j.parts - 1) / j.parts + 1) & ~1, from = j.part * share, to = min(rows, from + share);   // (pairs stay together)
+  const long long apart = (long long)a.Hkv * R, slot = (long long)(blockIdx.x - j.part * a.Hkv) * R;
+  for (int r0 = from; r0 < to; r0 += kEach) {
+    const int at = r0 + (threadIdx.x >> 4), r = min(at, to - 1);
+    const float2 *ml = a.ml + slot + r;
+    const float *o = a.o + (slot + r) * D + d;
+    float M = -INFINITY, l = 0.f;
+    for (int p = 0; p < j.parts; ++p) M = fmaxf(M, ml[p * apart].x);
+    float4 y[D / 64];
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < j.parts; ++p) {
+      const float2 s = ml[p * apart];
+      const float f = pg_weight(s.x, M);
+      l = f == 0.f ? l : fmaf(f, s.y, l);
+#pragma unroll
+      for (int q = 0; q < D / 64; ++q) {
+        const float4 x = *(const float4 *)(o + p * apart * D + 64 * q);
+        pg_add4(y[q], f, x);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, at < to ? first_row + at : 0x7fffffff, d + 64 * q, y[q], 1.f / l);
   }
 }
 
@@ -882,22 +940,28 @@ constexpr int kManySlots = 256, kFewSlots = kPagesCounters;
 constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
 size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
 
-template <int R, typename Kernel>
-static void launch_blocks(PagesLaunch a, Kernel kernel, int threads, int slots, float *scratch, hipStream_t stream) {
+// The launch's slots, and the workgroups it has.
+template <int R>
+static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, float *scratch) {
   // Blocks that there can be at most; fewer than the slots: the call may be split.  Without counts of their own all sequences
   // have `tokens` each: the blocks are known, and where they fill the slots none is cut.
   const long long most = (long long)a.B * (((long long)a.tokens * a.G + R - 1) / R) * a.Hkv;
-  a.slots = scratch && (a.count || most <= slots) ? slots : 0;
+  const bool may_split = scratch && (long long)a.pages.max_pages << a.pages.lg > least_part && (a.count || most <= slots);
+  a.slots = may_split ? slots : 0;
   a.ml = (float2 *)scratch;
   a.o = scratch + kSlotRows * 2;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)std::max<long long>(most, a.slots)), dim3(threads), 0, stream, a);
+  return (unsigned)std::max<long long>(most, a.slots);
 }
 template <int D>
-static void launch_pages_of(const PagesLaunch &a, float *scratch, hipStream_t stream) {
-  if ((long long)a.tokens * a.G <= kPgRows)
-    launch_blocks<kPgRows>(a, pages_few_kernel<D>, kFewWaves * kWave, kFewSlots, scratch, stream);
-  else
-    launch_blocks<kManyRows>(a, pages_many_kernel<D>, kManyThreads, kManySlots, scratch, stream);
+static void launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
+  if ((long long)a.tokens * a.G <= kPgRows) {
+    const unsigned grid = plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, scratch);
+    hipLaunchKernelGGL(pages_few_kernel<D>, dim3(grid), dim3(kFewWaves * kWave), 0, stream, a);
+  } else {
+    const unsigned grid = plan_blocks<kManyRows>(a, kManySlots, kManyLeastPart, scratch);
+    hipLaunchKernelGGL(pages_many_kernel<D>, dim3(grid), dim3(kManyThreads), 0, stream, a);
+    if (a.slots) hipLaunchKernelGGL(pages_merge_kernel<D>, dim3(a.slots), dim3(kManyThreads), 0, stream, a);
+  }
 }
 hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream) {
   if ((long long)a.B * a.tokens * a.G / kPgRows * a.Hkv > 0x40000000ll) return hipErrorInvalidValue;
