@@ -89,6 +89,18 @@ __device__ __forceinline__ int pg_scan(int v) {
   return v;
 }
 __device__ __forceinline__ int pg_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
+// The largest of values that are not negative.
+__device__ __forceinline__ int pg_max(int v) {
+#define CONFKV_DPP(ctrl, rows) v = max(v, __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false))
+  CONFKV_DPP(0x111, 0xf);
+  CONFKV_DPP(0x112, 0xf);
+  CONFKV_DPP(0x114, 0xf);
+  CONFKV_DPP(0x118, 0xf);
+  CONFKV_DPP(0x142, 0xa);
+  CONFKV_DPP(0x143, 0xc);
+#undef CONFKV_DPP
+  return pg_last(v);
+}
 
 // Parts of equal length for all sequences, the shortest for which every (block, part) has a slot; the blocks of a
 // sequence from the last one on, whose rows see the most keys.  False: the workgroup has nothing to do.
@@ -112,7 +124,7 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
       const int n = blocks_of(q);
       blocks += pg_last(pg_scan(n));
       work += (float)pg_last(pg_scan((int)fminf((float)n * (float)length(q), 0x1p24f)));   // (an estimate to begin with)
-      longest = max(longest, (unsigned)wave_max((int)length(q)));
+      longest = max(longest, (unsigned)pg_max((int)length(q)));
     }
     if (blocks > 0 && (unsigned)blocks <= most) {
       part = max(pg_least_part<R, QUANTUM>(a, longest), (unsigned)(work / (float)most));
@@ -299,11 +311,11 @@ struct PgRows {
   // scores -> probabilities
   __device__ __forceinline__ void weights(const pg_f16 &sc, float c, pg_h8 (&pb)[2]) {
     const float at = off == INFINITY ? 0.f : off;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[4];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c, at));
-      sum[i & 3] += p;
+      sum[i & 3] = i < 4 ? p : sum[i & 3] + p;
       // (fp16 operands: half a step, 2^-11 of each probability)
       pb[i / 8][i & 7] = (_Float16)p;
     }
