@@ -188,7 +188,8 @@ typedef struct conf_kv_stats {
  * instead of the planned number (clamped to what the unit's length allows);
  * CONF_KV_TWO_LAUNCH=1 forces the two-launch form of conf_kv_attend; CONF_KV_SHARED_ROWS=1/2/4 the number of
  * wavefronts side by side along the rows of conf_kv_attend_shared's prefix kernel; CONF_KV_NO_MFMA=1 (read
- * at the first plan of the process) keeps every shape on the vector-ALU streaming body;
+ * at the first plan of the process) keeps every shape on the vector-ALU streaming body (conf_kv_attend_diff then has
+ * no kernel: CONF_KV_ERR_BAD_SHAPE);
  * CONF_KV_SPIN_LIMIT=n bounds the in-kernel waits for other workgroups to n polls (default
  * 400000, about 0.4 s; an expired wait ends the kernel early and counts a device error);
  * CONF_KV_TEST_WITHHOLD=1 makes split 0 of every unit (conf_kv_attend) and chunk 0 of every
@@ -315,7 +316,6 @@ int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const co
  * of a call as in conf_kv_attend_chunk).  Tensors, errors and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend) but for dev_out16,
  * fp16 [B][tq][Hq / 2][D], and dev_lambda, fp32 [B][tq][Hq / 2] with sequences batch_stride and tokens token_stride values apart
  * (0: the same weights for all).  An odd group or tq * n_q_heads / n_kv_heads above 16 is CONF_KV_ERR_INVALID_ARG.
- * The norm of the outputs' heads that such models put behind it is conf_kv_prepare_qkv's (dev_q alone, rotated = 0).
  * conf_kv_observe* see single maps: the importance they give sums to G per query, more than a step's here. */
 int conf_kv_attend_diff(conf_kv_handle *h, int32_t layer, int32_t tq, const float *dev_lambda, int64_t batch_stride,
                         int64_t token_stride, const void *dev_q16, const void *dev_knew16, const void *dev_vnew16, void *dev_out16,

@@ -767,14 +767,14 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   const int lrow = RWI * w + lane / PR, lpiece = (lane % PR) ^ pg_swizzle<D>(lrow);
   const long long lane_off = (lane / PR) * src.token_stride + lpiece * 8;
   const unsigned page_lane = (unsigned)(2 * lane_off), new_lane = (unsigned)(2 * ((lane / PR) * src.new_stride + lpiece * 8));
-  const bool near = src.token_stride < 1 << 26;          // (a wavefront's rows of a page less than 2^32 bytes apart)
+  const bool near = src.token_stride < 1 << 26 && src.new_stride < 1 << 26;   // (a wavefront's rows less than 2^32 bytes apart)
   const unsigned lds0 = pg_lds_at(s_tile);
   int ent = src.entry(lo + lane);
   auto issue = [&](int t, int buffer) {                  // (every tile's entries were requested with the tile before)
     if (t >= tiles) return;
     const int base = lo + t * kManyKeys;
     const unsigned to = lds0 + buffer * M::kBuffer + RWI * w * ROW;
-    if (base >= src.c && base + kManyKeys <= src.n) {    // nothing but tokens of the call
+    if (base >= src.c && base + kManyKeys <= src.n && near) {   // nothing but tokens of the call
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const long long m = (base + RPP * i + RWI * w - src.c) * src.new_stride;
@@ -952,34 +952,36 @@ constexpr int kManySlots = 256, kFewSlots = kPagesCounters;
 constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
 size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
 
-// The launch's slots, and the workgroups it has.
+// The launch's slots, and the workgroups it has: no more than there can be blocks, a sequence's last one apart (rows belong to one
+// sequence), and one per slot where the call may be split.  Without counts of their own all sequences have `tokens` each: the blocks
+// are known, and where they fill the slots none is cut.  0: too many for a launch.
 template <int R>
-static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, float *scratch) {
-  // Blocks that there can be at most; fewer than the slots: the call may be split.  Without counts of their own all sequences
-  // have `tokens` each: the blocks are known, and where they fill the slots none is cut.
-  const long long most = (long long)a.B * (((long long)a.tokens * a.G + R - 1) / R) * a.Hkv;
-  const bool may_split = scratch && (long long)a.pages.max_pages << a.pages.lg > least_part && (a.count || most <= slots);
+static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, int threads, float *scratch) {
+  const long long each = ((long long)a.tokens * a.G + R - 1) / R;
+  const long long most = a.Hkv * std::min(a.B * each, (long long)a.rows * a.G / R + a.B);
+  const bool may_split = scratch && (long long)a.pages.max_pages << a.pages.lg > least_part && (a.count || a.B * each * a.Hkv <= slots);
   a.slots = may_split ? slots : 0;
   a.ml = (float2 *)scratch;
   a.o = scratch + kSlotRows * 2;
-  return (unsigned)std::max<long long>(most, a.slots);
+  const long long grid = std::max<long long>(most, a.slots);
+  return grid * threads < 1ll << 32 ? (unsigned)grid : 0u;
 }
 template <int D>
-static void launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
-  if ((long long)a.tokens * a.G <= kPgRows) {
-    const unsigned grid = plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, scratch);
+static hipError_t launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
+  const bool few = (long long)a.tokens * a.G <= kPgRows;
+  const unsigned grid = few ? plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, kFewWaves * kWave, scratch)
+                            : plan_blocks<kManyRows>(a, kManySlots, kManyLeastPart, kManyThreads, scratch);
+  if (grid == 0) return hipErrorInvalidValue;
+  if (few) {
     hipLaunchKernelGGL(pages_few_kernel<D>, dim3(grid), dim3(kFewWaves * kWave), 0, stream, a);
   } else {
-    const unsigned grid = plan_blocks<kManyRows>(a, kManySlots, kManyLeastPart, scratch);
     hipLaunchKernelGGL(pages_many_kernel<D>, dim3(grid), dim3(kManyThreads), 0, stream, a);
     if (a.slots) hipLaunchKernelGGL(pages_merge_kernel<D>, dim3(a.slots), dim3(kManyThreads), 0, stream, a);
   }
+  return hipGetLastError();
 }
 hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream) {
-  if ((long long)a.B * a.tokens * a.G / kPgRows * a.Hkv > 0x40000000ll) return hipErrorInvalidValue;
-  if (D == 64) launch_pages_of<64>(a, scratch, stream);
-  else launch_pages_of<128>(a, scratch, stream);
-  return hipGetLastError();
+  return D == 64 ? launch_pages_of<64>(a, scratch, stream) : launch_pages_of<128>(a, scratch, stream);
 }
 
 }  // namespace confkv
