@@ -23,6 +23,8 @@ typedef float pg_f16 __attribute__((ext_vector_type(16)));
 constexpr int kPgKeys = 32;                            // keys of a wavefront's tile
 constexpr int kPgRows = 32;                            // rows of a matrix instruction's tile
 constexpr int kNoSplit = 0x7fffffff;
+constexpr int kFewWaves = 4, kFewQuantum = kFewWaves * kPgKeys;   // few rows: wavefronts, and keys that a part has at least
+static_assert(kFewQuantum == kPagesLeastPart);
 
 // Per group of sixteen lanes: lane l reads four halfs of row l / 4, columns 4 (l & 3) + [0, 4), and gets half l of each row.
 __device__ __forceinline__ pg_h4 pg_read_tr(const uint8_t *p) {
@@ -66,15 +68,16 @@ struct PgJob {
   int b, g, block, part, parts, part_keys;
   PgSequence q;
 };
-// The least quanta that a part has.  Few rows: the workgroup that merges the parts, alone, reads as many bytes for every row of every
-// part as for a key, so that with parts shorter than the square root of keys * rows the merge would take longer than a part.
-// Many rows: 512 keys take as long (18 us) as the merge's launch twice.
-constexpr int kManyLeastPart = 512;
+// The least quanta that a part has.  Few rows: a part takes 10 ns for each of its keys, and the workgroup that merges the parts, alone,
+// some 19 ns for each row of each; the sum is least with parts of sqrt(1.9 keys rows).
+// Many rows: 256 keys, of caches of 512 and more (us with parts of 256, 512, 1024: 64 rows behind 2000 tokens 19.5, 25.0, 37.9, 256 behind
+// 500 22.6, 30.1, 27.2, 1024 behind 2000 32.7, 35.2, 47.4; four sequences of 333 tokens, uncut 14.5, in halves 23.5).
+constexpr int kManyLeastPart = 256;
 template <int R, int QUANTUM>
 __device__ __forceinline__ unsigned pg_least_part(const PagesLaunch &a, unsigned longest) {
-  if constexpr (R != kPgRows) return kManyLeastPart / QUANTUM;
+  if constexpr (R != kPgRows) return (longest * QUANTUM < 2 * kManyLeastPart ? longest : kManyLeastPart / QUANTUM);
   const float rows = (float)min((long long)a.tokens * a.G, (long long)R);
-  return max(1u, (unsigned)(__builtin_sqrtf((float)longest * QUANTUM * rows) * (1.f / QUANTUM)));
+  return max(1u, (unsigned)(__builtin_sqrtf((float)longest * QUANTUM * rows * 1.9f) * (1.f / QUANTUM) + 0.5f));
 }
 // Inclusive prefix sums over the wavefront by lane moves (an exchange through LDS takes ten times as long).
 __device__ __forceinline__ int pg_scan(int v) {
@@ -467,8 +470,9 @@ struct PgParts {
     pg_store8(to + 2, y.z, y.w);
   }
   static __device__ __forceinline__ void store_sums(const PagesLaunch &a, int row, float m, float l) { pg_store8((float *)(a.ml + at(row)), m, l); }
-  // Behind the stores, all threads of the workgroup.
-  static __device__ __forceinline__ void merge(const PagesLaunch &a, const PgJob &j, int threads) {
+  // Behind the stores, all threads of the workgroup; `room` is kRoom floats of LDS that nobody uses any more.
+  static constexpr int kGroups = kFewWaves * kWave / 16, kSlot = D + 4, kRoom = R * kSlot;
+  static __device__ __forceinline__ void merge(const PagesLaunch &a, const PgJob &j, float *room) {
     __shared__ int s_last;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -480,64 +484,80 @@ struct PgParts {
     }
     __syncthreads();
     if (!s_last) return;
-    const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row), d = (threadIdx.x & 15) * 4, each = threads / 16;
+    // Groups of sixteen threads.  Where there are fewer rows than groups, 2^lg of them share a row, each with parts of its own.
+    const int first_row = j.block * R, rows = min(R, j.q.n * a.G - first_row), d = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
+    int lg = 0;
+    while ((2 << lg) * rows <= kGroups) ++lg;
+    const int mate = group & ((1 << lg) - 1), each = kGroups >> lg;
     const long long apart = (long long)a.Hkv * R;
-    constexpr int kSide = 2, kAhead = 4;                 // rows of a thread, parts whose words are requested together
-    for (int r0 = 0; r0 < rows; r0 += kSide * each) {
-      const float *ml[kSide], *o[kSide];
-      float M[kSide], l[kSide];
-      float4 y[kSide][D / 64];
+    auto clear = [](float4 (&y)[D / 64], float &l) {
 #pragma unroll
-      for (int i = 0; i < kSide; ++i) {
-        const long long r = (long long)first * R + min(r0 + i * each + (int)(threadIdx.x >> 4), R - 1);   // (past the last row: what nothing reads)
-        ml[i] = (const float *)(a.ml + r);
-        o[i] = a.o + r * D + d;
-        M[i] = -INFINITY;
-        l[i] = 0.f;
+      for (int q = 0; q < D / 64; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      l = 0.f;
+    };
+    for (int r0 = 0, slot = group; r0 < rows; r0 += each, slot += kGroups) {
+      const int r = min(r0 + (group >> lg), rows - 1);
+      const float *ml = (const float *)(a.ml + (long long)first * R + r);
+      const float *o = a.o + ((long long)first * R + r) * D + d;
+      float M = -INFINITY, l;
+      float4 y[D / 64];
+      clear(y, l);
+      constexpr int kAhead = 8;                          // parts whose words are requested together
+      for (int p0 = mate; p0 < j.parts; p0 += kAhead << lg) {
+        float2 s[kAhead], x[kAhead][D / 64][2];
 #pragma unroll
-        for (int q = 0; q < D / 64; ++q) y[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      for (int p0 = 0; p0 < j.parts; p0 += kAhead) {
-        float2 s[kSide][kAhead], x[kSide][kAhead][D / 64][2];
-#pragma unroll
-        for (int i = 0; i < kSide; ++i)
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            const long long p = min(p0 + k, j.parts - 1) * apart;
-            s[i][k] = pg_load8(ml[i] + 2 * p);
-#pragma unroll
-            for (int q = 0; q < D / 64; ++q) {
-              x[i][k][q][0] = pg_load8(o[i] + p * D + 64 * q);
-              x[i][k][q][1] = pg_load8(o[i] + p * D + 64 * q + 2);
-            }
-          }
-#pragma unroll
-        for (int i = 0; i < kSide; ++i) {
-          float now = M[i];
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) now = fmaxf(now, s[i][k].x);
-          const float f0 = pg_weight(M[i], now);
-          l[i] = f0 == 0.f ? 0.f : l[i] * f0;
+        for (int k = 0; k < kAhead; ++k) {
+          const long long p = min(p0 + (k << lg), j.parts - 1) * apart;
+          s[k] = pg_load8(ml + 2 * p);
 #pragma unroll
           for (int q = 0; q < D / 64; ++q) {
-            const float4 was = y[i][q];
-            y[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
-            pg_add4(y[i][q], f0, was);
+            x[k][q][0] = pg_load8(o + p * D + 64 * q);
+            x[k][q][1] = pg_load8(o + p * D + 64 * q + 2);
           }
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            const float f = p0 + k < j.parts ? pg_weight(s[i][k].x, now) : 0.f;
-            l[i] = f == 0.f ? l[i] : fmaf(f, s[i][k].y, l[i]);
-#pragma unroll
-            for (int q = 0; q < D / 64; ++q) pg_add4(y[i][q], f, make_float4(x[i][k][q][0].x, x[i][k][q][0].y, x[i][k][q][1].x, x[i][k][q][1].y));
-          }
-          M[i] = now;
         }
+        float now = M;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) now = fmaxf(now, s[k].x);
+        const float f0 = pg_weight(M, now), was = l;
+        float4 old[D / 64];
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) old[q] = y[q];
+        clear(y, l);
+        l = f0 == 0.f ? l : was * f0;
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f0, old[q]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float f = p0 + (k << lg) < j.parts ? pg_weight(s[k].x, now) : 0.f;
+          l = f == 0.f ? l : fmaf(f, s[k].y, l);
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f, make_float4(x[k][q][0].x, x[k][q][0].y, x[k][q][1].x, x[k][q][1].y));
+        }
+        M = now;
+      }
+      if (slot < R) {
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) *(float4 *)(room + slot * kSlot + d + 64 * q) = y[q];
+        if (d == 0) *(float2 *)(room + slot * kSlot + D) = make_float2(M, l);
+      }
+    }
+    __syncthreads();
+    for (int r0 = 0; r0 < rows; r0 += kGroups) {
+      const int row = r0 + group, r = min(row, rows - 1);
+      const float *mine = room + (r / each * kGroups + ((r & (each - 1)) << lg)) * kSlot;
+      float M = -INFINITY, l;
+      float4 y[D / 64];
+      clear(y, l);
+      for (int k = 0; k < 1 << lg; ++k) M = fmaxf(M, mine[k * kSlot + D]);
+      for (int k = 0; k < 1 << lg; ++k) {
+        const float2 s = *(const float2 *)(mine + k * kSlot + D);
+        const float f = pg_weight(s.x, M);
+        l = f == 0.f ? l : fmaf(f, s.y, l);
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f, *(const float4 *)(mine + k * kSlot + d + 64 * q));
       }
 #pragma unroll
-      for (int i = 0; i < kSide; ++i)
-#pragma unroll
-        for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + r0 + i * each + (int)(threadIdx.x >> 4), d + 64 * q, y[i][q], 1.f / l[i]);
+      for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + row, d + 64 * q, y[q], 1.f / l);
     }
   }
 };
@@ -574,8 +594,6 @@ struct PgTile {
 // next one in flight in registers while this one is used.
 // ---------------------------------------------------------------------------------------
 constexpr int kManyQuantum = 64;
-constexpr int kFewWaves = 4, kFewQuantum = kFewWaves * kPgKeys;
-static_assert(kFewQuantum == kPagesLeastPart);
 
 template <int D>
 __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void pages_few_kernel(PagesLaunch a) {
@@ -674,7 +692,8 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   }
   if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D>::store_sums(a, row, M, l);
   }
-  if (j.parts > 1) PgParts<D>::merge(a, j, kFewWaves * kWave);
+  if (j.parts > 1) PgParts<D>::merge(a, j, (float *)s_tile);
+  static_assert(PgParts<D>::kRoom * 4 <= sizeof(s_tile));
 }
 
 // ---------------------------------------------------------------------------------------
@@ -948,7 +967,7 @@ __global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a
 // ---------------------------------------------------------------------------------------
 // Slots of a split call, by the rows of a block: a workgroup of many rows per compute unit; of few rows, whose sequences may be of any
 // length, some more, so that no part is much longer than the others.
-constexpr int kManySlots = 256, kFewSlots = kPagesCounters;
+constexpr int kManySlots = 256, kFewSlots = 512;
 constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
 size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
 
@@ -970,7 +989,7 @@ template <int D>
 static hipError_t launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
   const bool few = (long long)a.tokens * a.G <= kPgRows;
   const unsigned grid = few ? plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, kFewWaves * kWave, scratch)
-                            : plan_blocks<kManyRows>(a, kManySlots, kManyLeastPart, kManyThreads, scratch);
+                            : plan_blocks<kManyRows>(a, kManySlots, 2 * kManyLeastPart - kManyKeys, kManyThreads, scratch);
   if (grid == 0) return hipErrorInvalidValue;
   if (few) {
     hipLaunchKernelGGL(pages_few_kernel<D>, dim3(grid), dim3(kFewWaves * kWave), 0, stream, a);

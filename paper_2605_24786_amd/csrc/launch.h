@@ -173,7 +173,7 @@ struct PagesLaunch {
   float *o;
   unsigned *arrived;                       // [kPagesCounters], zero between calls: parts of a block that have left their results
 };
-constexpr int kPagesCounters = 1024;
+constexpr int kPagesCounters = 512;
 size_t pages_scratch_floats(int D);
 hipError_t launch_pages(const PagesLaunch &a, int D, float *scratch, hipStream_t stream);
 // Importance of a freshly loaded prompt of T tokens from all its queries q [B][T][Hq][D] (D = 128,
