@@ -64,6 +64,9 @@ __device__ __forceinline__ PgSequence pg_sequence(const PagesLaunch &a, int b) {
   return q;
 }
 
+// Token of a sequence's row (a division by the group size; a multiplier of 0: groups of one).
+__device__ __forceinline__ int pg_token(const PagesLaunch &a, int row) { return a.g_magic ? (int)(__umulhi((unsigned)row, a.g_magic) >> a.g_shift) : row; }
+
 struct PgJob {
   int b, g, block, part, parts, part_keys;
   PgSequence q;
@@ -264,7 +267,7 @@ struct PgRows {
     const int lane = threadIdx.x & 63, h = lane >> 5, all = j.q.n * a.G;
     row = first + (lane & 31);
     const bool real = row < all;
-    const int r = min(row, all - 1), t = r / a.G, hq = r - t * a.G;
+    const int r = min(row, all - 1), t = pg_token(a, r), hq = r - t * a.G;
     const __half *q = a.q + ((long long)(j.q.s + t) * a.Hkv * a.G + j.g * a.G + hq) * D;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) qf[s] = __builtin_bit_cast(pg_h8, *(const int4 *)(q + 16 * s + 8 * h));
@@ -406,18 +409,6 @@ struct PgRows {
   }
 };
 
-// The weight of the second map of pair row / 2 where heads are subtracted (a row is a first map's where it is even).
-__device__ __forceinline__ float pg_lambda(const PagesLaunch &a, const PgJob &j, int row) {
-  const int t = row / a.G, pair = (row - t * a.G) >> 1;
-  return a.lambda[(j.q.s + t) * a.lambda_stride + j.g * (a.G >> 1) + pair];
-}
-// Where row `row` of the sequence goes: [rows][heads][D], half of the heads where they are subtracted in pairs.
-template <int D>
-__device__ __forceinline__ __half *pg_out_row(const PagesLaunch &a, const PgJob &j, int row) {
-  const int t = row / a.G, hq = row - t * a.G, G = a.lambda ? a.G >> 1 : a.G;
-  return a.out + (((long long)(j.q.s + t) * a.Hkv + j.g) * G + (a.lambda ? hq >> 1 : hq)) * D;
-}
-
 // Weight of a partial result with maximum m beside one of maximum M.
 __device__ __forceinline__ float pg_weight(float m, float M) {
   return m == -INFINITY ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m - M), kLeastWeight);
@@ -430,22 +421,32 @@ __device__ __forceinline__ void pg_add4(float4 &y, float f, const float4 &x) {
   y.z = some ? fmaf(f, x.z, y.z) : y.z;
   y.w = some ? fmaf(f, x.w, y.w) : y.w;
 }
-// Channels d .. d + 3 of row `row`, sums y over its normaliser; sixteen neighbouring lanes hold a row, the next sixteen the next one.
-// Heads that are subtracted in pairs: the even row takes the odd one's from there.  (All lanes call it.)
+// Where row `row` of the sequence goes, [rows][heads][D]: nowhere behind the last one, and where heads are subtracted in pairs, odd
+// rows into their pair's with the weight f.
+struct PgOut {
+  __half *at;
+  float f;
+};
 template <int D>
-__device__ __forceinline__ void pg_write_out(const PagesLaunch &a, const PgJob &j, int row, int d, float4 y, float inv) {
+__device__ __forceinline__ PgOut pg_out(const PagesLaunch &a, const PgJob &j, int row) {
+  const int r = min(row, j.q.n * a.G - 1), t = pg_token(a, r), hq = r - t * a.G;
+  const long long token = j.q.s + t;
+  if (!a.lambda) return {row == r ? a.out + ((token * a.Hkv + j.g) * a.G + hq) * D : nullptr, 0.f};
+  const int half = a.G >> 1, pair = hq >> 1;
+  return {row == r && (hq & 1) == 0 ? a.out + ((token * a.Hkv + j.g) * half + pair) * D : nullptr, a.lambda[token * a.lambda_stride + j.g * half + pair]};
+}
+// Channels d .. d + 3 of a row, sums y over its normaliser; sixteen neighbouring lanes hold a row, the next sixteen the next one.
+// (All lanes call it.)
+__device__ __forceinline__ void pg_write_out(const PagesLaunch &a, const PgOut &to, int d, float4 y, float inv) {
   y.x *= inv;
   y.y *= inv;
   y.z *= inv;
   y.w *= inv;
-  const bool real = row < j.q.n * a.G;
   if (a.lambda) {
     const float4 z = make_float4(__shfl_xor(y.x, 16, kWave), __shfl_xor(y.y, 16, kWave), __shfl_xor(y.z, 16, kWave), __shfl_xor(y.w, 16, kWave));
-    if (!real || (row & 1)) return;
-    const float f = pg_lambda(a, j, row);
-    y = make_float4(fmaf(-f, z.x, y.x), fmaf(-f, z.y, y.y), fmaf(-f, z.z, y.z), fmaf(-f, z.w, y.w));
+    y = make_float4(fmaf(-to.f, z.x, y.x), fmaf(-to.f, z.y, y.y), fmaf(-to.f, z.z, y.z), fmaf(-to.f, z.w, y.w));
   }
-  if (real) *(pg_h4 *)(pg_out_row<D>(a, j, row) + d) = pg_h4{(_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
+  if (to.at) *(pg_h4 *)(to.at + d) = pg_h4{(_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
 }
 
 // ---------------------------------------------------------------------------------------
@@ -556,8 +557,9 @@ struct PgParts {
 #pragma unroll
         for (int q = 0; q < D / 64; ++q) pg_add4(y[q], f, *(const float4 *)(mine + k * kSlot + d + 64 * q));
       }
+      const PgOut to = pg_out<D>(a, j, first_row + row);
 #pragma unroll
-      for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, first_row + row, d + 64 * q, y[q], 1.f / l);
+      for (int q = 0; q < D / 64; ++q) pg_write_out(a, to, d + 64 * q, y[q], 1.f / l);
     }
   }
 };
@@ -567,7 +569,7 @@ template <int D>
 __device__ __forceinline__ void pg_append(const PagesLaunch &a, const PgJob &j, int lo, int hi, int threads) {
   if (!a.knew || j.part != 0) return;
   constexpr int PR = D / 8;
-  const int t0 = (lo + a.G - 1) / a.G, t1 = min(j.q.n, (hi + a.G - 1) / a.G);
+  const int t0 = pg_token(a, lo + a.G - 1), t1 = min(j.q.n, pg_token(a, hi + a.G - 1));
   for (int i = threadIdx.x; i < (t1 - t0) * PR; i += threads) {
     const int t = t0 + i / PR, at = j.q.c + t;
     const int e = a.pages.table[j.b * a.pages.table_stride + (at >> a.pages.lg)];
@@ -670,6 +672,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   const int rows = min(kPgRows, j.q.n * a.G - first_row);
   for (int r0 = 0; r0 < rows; r0 += kFewWaves * 4) {
   const int row = r0 + (tid >> 4);
+  const PgOut to = pg_out<D>(a, j, first_row + row);
   float m[kFewWaves], M = -INFINITY, l = 0.f;
 #pragma unroll
   for (int k = 0; k < kFewWaves; ++k) {
@@ -687,7 +690,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
-    if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / l);
+    if (j.parts == 1) pg_write_out(a, to, d, y, 1.f / l);
     else if (row < rows) PgParts<D>::store(a, row, d, y);
   }
   if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D>::store_sums(a, row, M, l);
@@ -777,9 +780,9 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   src.init(a, j);
   const int first_row = j.block * R, last_row = min(first_row + R, j.q.n * a.G) - 1;
   const int lo = j.parts > 1 ? j.part * j.part_keys : 0;
-  const int seen = j.q.c + last_row / a.G + 1;           // keys that the block's last row sees
+  const int seen = j.q.c + pg_token(a, last_row) + 1;    // keys that the block's last row sees
   const int hi = (int)min((long long)lo + j.part_keys, (long long)seen);
-  const int all_least = j.q.c + first_row / a.G + 1;     // and its first one
+  const int all_least = j.q.c + pg_token(a, first_row) + 1;   // and its first one
   const int tiles = hi > lo ? (hi - lo + kManyKeys - 1) / kManyKeys : 0;
   const int full = max(0, (min(all_least, hi) - lo) / kManyKeys);   // tiles that every row sees to the end
   // The lane's row and piece of a wavefront's load; f does not depend on which of a tile's loads it is.
@@ -904,6 +907,13 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   float *wo = (float *)s_tile + w * kPgRows * 64;
   const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l);
   const int l32 = lane & 31, h = lane >> 5;
+  PgOut to[kPgRows / 4];
+  float inv[kPgRows / 4];
+#pragma unroll
+  for (int p = 0; p < kPgRows / 4; ++p) {
+    to[p] = pg_out<D>(a, j, first_row + w * kPgRows + 4 * p + (lane >> 4));
+    inv[p] = 1.f / __shfl(l, 4 * p + (lane >> 4), kWave);
+  }
 #pragma unroll
   for (int q = 0; q < D / 64; ++q) {
 #pragma unroll
@@ -917,9 +927,8 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
 #pragma unroll
     for (int p = 0; p < kPgRows / 4; ++p) {
       const int r = 4 * p + (lane >> 4), row = w * kPgRows + r, d = (lane & 15) * 4 + 64 * q;
-      const float lr = __shfl(l, r, kWave);
       const float4 y = *(const float4 *)(wo + r * 64 + (((lane & 15) ^ (r & 15)) << 2));
-      if (j.parts == 1) pg_write_out<D>(a, j, first_row + row, d, y, 1.f / lr);
+      if (j.parts == 1) pg_write_out(a, to[p], d, y, inv[p]);
       else if (first_row + row <= last_row) *(float4 *)(a.o + ((long long)blockIdx.x * R + row) * D + d) = y;
     }
     pg_wave_sync();
@@ -957,8 +966,9 @@ __global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a
         pg_add4(y[q], f, x);
       }
     }
+    const PgOut place = pg_out<D>(a, j, at < to ? first_row + at : kNoSplit);
 #pragma unroll
-    for (int q = 0; q < D / 64; ++q) pg_write_out<D>(a, j, at < to ? first_row + at : 0x7fffffff, d + 64 * q, y[q], 1.f / l);
+    for (int q = 0; q < D / 64; ++q) pg_write_out(a, place, d + 64 * q, y[q], 1.f / l);
   }
 }
 
@@ -988,6 +998,7 @@ static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, int threa
 template <int D>
 static hipError_t launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
   const bool few = (long long)a.tokens * a.G <= kPgRows;
+  a.g_magic = a.G > 1 ? split_divisor(a.G, &a.g_shift) : 0u;
   const unsigned grid = few ? plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, kFewWaves * kWave, scratch)
                             : plan_blocks<kManyRows>(a, kManySlots, 2 * kManyLeastPart - kManyKeys, kManyThreads, scratch);
   if (grid == 0) return hipErrorInvalidValue;

@@ -167,8 +167,10 @@ struct PagesLaunch {
   const float *lambda;                     // null, or weights [rows][Hkv * G / 2], rows lambda_stride apart
   long long lambda_stride;
   int B, Hkv, G;
+  unsigned g_magic;                        // a division by G (split_divisor), 0 for 1; filled in by the launcher, as all below
+  int g_shift;
   float sm_scale;
-  int slots;                               // (block, part) pairs of a split call at most; filled in by the launcher, as ml and o
+  int slots;                               // (block, part) pairs of a split call at most
   float2 *ml;
   float *o;
   unsigned *arrived;                       // [kPagesCounters], zero between calls: parts of a block that have left their results
