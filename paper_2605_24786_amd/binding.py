@@ -300,21 +300,19 @@ class ConfKV:
 
     def _pages(self, pages_k, pages_v, table):
         """conf_kv_pages of two float16 tensors [pages][page][Hkv][D] and an int32 table [B][pages per sequence]."""
-        B, H, D, half, device = self._batch, self._kv_heads, self._head_dim, self._half, self._device
+        B, half, device = self._batch, self._half, self._device
         shape, apart = pages_k.shape, pages_k.stride()
-        if (len(shape) != 4 or shape[2:] != (H, D) or pages_k.dtype is not half or pages_k.get_device() != device or
-                pages_v.shape != shape or pages_v.dtype is not half or pages_v.get_device() != device or apart[3] != 1 or
-                pages_v.stride() != apart):
-            raise ValueError(f"pages_k, pages_v: float16 [pages][page][{H}][{D}] with dense heads and equal strides on "
-                             f"{self.state.device} are wanted, got {pages_k.dtype} {tuple(shape)} {apart} and {pages_v.dtype} "
-                             f"{tuple(pages_v.shape)} {pages_v.stride()} on {pages_k.device} and {pages_v.device}")
-        rows = table.shape
-        step = table.stride()
-        if len(rows) != 2 or rows[0] != B or table.dtype is not self._i32 or table.get_device() != device or (rows[1] > 1 and step[1] != 1):
-            raise ValueError(f"table: int32 [{B}][pages per sequence] with dense rows on {self.state.device} is wanted, got {table.dtype} "
-                             f"{tuple(rows)} {step} on {table.device}")
-        return _PAGES.pack(pages_k.data_ptr(), pages_v.data_ptr(), apart[0], apart[1], apart[2], shape[1], shape[0], table.data_ptr(),
-                           step[0] if B > 1 else rows[1], rows[1])
+        rows, step = table.shape, table.stride()
+        if (len(shape) == 4 and shape[2] == self._kv_heads and shape[3] == self._head_dim and apart[3] == 1 and pages_k.dtype is half and
+                pages_v.dtype is half and pages_v.shape == shape and pages_v.stride() == apart and pages_k.get_device() == device and
+                pages_v.get_device() == device and len(rows) == 2 and rows[0] == B and table.dtype is self._i32 and
+                table.get_device() == device and (step[1] == 1 or rows[1] == 1)):
+            return _PAGES.pack(pages_k.data_ptr(), pages_v.data_ptr(), apart[0], apart[1], apart[2], shape[1], shape[0], table.data_ptr(),
+                               step[0] if B > 1 else rows[1], rows[1])
+        raise ValueError(f"pages_k, pages_v: float16 [pages][page][{self._kv_heads}][{self._head_dim}] with dense heads and equal strides, and "
+                         f"table: int32 [{B}][pages per sequence] with dense rows, on {self.state.device} are wanted, got {pages_k.dtype} "
+                         f"{tuple(shape)} {apart}, {pages_v.dtype} {tuple(pages_v.shape)} {pages_v.stride()}, {table.dtype} {tuple(rows)} "
+                         f"{step} on {pages_k.device}, {pages_v.device}, {table.device}")
 
     def attend_pages(self, q16, knew16, vnew16, out16, pages_k, pages_v, table, context, tokens=None, starts=None, new=None, lam=None):
         """New tokens of every sequence over a paged cache pages_k, pages_v float16 [pages][page][Hkv][D] (any order of the dimensions
@@ -322,31 +320,31 @@ class ConfKV:
         q16 [B][T][Hq][D], knew16 / vnew16 [B][T][Hkv][D] (None: the pages hold them); or rows [R][..][D] of which sequence b has
         starts[b] .. starts[b] + new[b] - 1 (int32 [B]), at most `tokens` of them.  out16 [..][Hq][D], with
         lam float32 [..][Hq / 2] or [Hq / 2], the weights of the second maps, [..][Hq / 2][D]."""
-        H, Hq, D, want, half, i32 = self._kv_heads, self._q_heads, self._head_dim, self._want, self._half, self._i32
-        lead = q16.shape[:-2]
-        rows = 1
-        for n in lead:
-            rows *= n
-        if len(lead) == 2:
-            tokens = lead[1] if tokens is None else tokens
-            if lead[0] != self._batch or tokens > lead[1]:
-                raise ValueError(f"q16: [{self._batch}][T][{Hq}][{D}] is wanted, got {tuple(q16.shape)} with {tokens} tokens")
-            if starts is None and tokens != lead[1]:
-                raise ValueError("tokens: fewer than the rows of a sequence need `starts`")
-        elif len(lead) != 1 or starts is None or tokens is None:
-            raise ValueError("q16: [B][T][Hq][D], or [R][Hq][D] with `starts` and `tokens`, is wanted")
-        row = (self._batch,)
+        B, H, Hq, D, want, half, i32 = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._want, self._half, self._i32
+        shape = q16.shape
         outs, weights, apart = Hq, 0, 0
         if lam is not None:
             outs = Hq // 2
+        if len(shape) == 3 and starts is not None and tokens is not None:
+            rows = shape[0]
+            like, fresh, given = (rows, Hq, D), (rows, H, D), (rows, outs, D)
+        elif len(shape) == 4 and shape[0] == B and (tokens is None or tokens == shape[1] or starts is not None and tokens < shape[1]):
+            T = shape[1]
+            rows = B * T
+            like, fresh, given = (B, T, Hq, D), (B, T, H, D), (B, T, outs, D)
+            if tokens is None:
+                tokens = T
+        else:
+            raise ValueError(f"q16: [{B}][T][{Hq}][{D}], with `starts` for fewer tokens than T, or [R][{Hq}][{D}] with `starts` and `tokens` "
+                             f"is wanted, got {tuple(shape)} with {tokens} tokens")
+        if lam is not None:
             if lam.shape == (outs,):
                 weights = want("lam", lam, self._f32, (outs,))
             else:
-                weights, apart = want("lam", lam, self._f32, (*lead, outs)), outs
-        fresh = (*lead, H, D)
-        chunk = _CHUNK.pack(tokens, rows, want("starts", starts, i32, row), want("new", new, i32, row), want("context", context, i32, row),
-                            want("q16", q16, half, (*lead, Hq, D)), want("knew16", knew16, half, fresh), want("vnew16", vnew16, half, fresh),
-                            want("out16", out16, half, (*lead, outs, D)), weights, apart)
+                weights, apart = want("lam", lam, self._f32, given[:-1]), outs
+        chunk = _CHUNK.pack(tokens, rows, want("starts", starts, i32, (B,)), want("new", new, i32, (B,)), want("context", context, i32, (B,)),
+                            want("q16", q16, half, like), want("knew16", knew16, half, fresh), want("vnew16", vnew16, half, fresh),
+                            want("out16", out16, half, given), weights, apart)
         return self._check(self.lib.conf_kv_attend_pages(self.h, self._pages(pages_k, pages_v, table), chunk, self._current_stream()),
                            "conf_kv_attend_pages")
 

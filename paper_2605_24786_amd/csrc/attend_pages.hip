@@ -2,8 +2,9 @@
 //
 // Rows of a kv-head are (token, head of the group), token first, so that all heads of the group share the tiles.  A workgroup takes
 // a block of rows of one (sequence, kv-head) against the keys those rows see, or against a part of them where there are fewer
-// blocks than compute units; parts leave float32 partial results which the last of them merges:
+// blocks than compute units; parts leave float32 partial results,
 //   ml[slot][row] = (m, l),  o[slot][row][D] = sum over the part's keys of 2^(s - m) v,   s: scores times log2(e)
+// which are merged in the order of the parts, whichever was there first.
 // Products are formed transposed, scores [32 keys x 32 rows] and output [D x 32 rows] (v_mfma_f32_32x32x16_f16): a lane then holds
 // values of one row only, its probabilities are the operand of the second product as they stand, and the row's statistics
 // need one exchange between two lanes.
@@ -593,7 +594,10 @@ struct PgTile {
 // ---------------------------------------------------------------------------------------
 // Up to 32 rows of a (sequence, kv-head), single tokens above all: bound by the bytes of K and V.  Four wavefronts take the
 // part's tiles of 32 keys in turn; a wavefront waits for nobody before the merge: it loads and multiplies tiles of its own, the
-// next one in flight in registers while this one is used.
+// next one in flight in registers while this one is used.  Two workgroups share a compute unit, so that one's first and last trips
+// to memory run beside the other's rows: 32 single tokens behind up to 8192 tokens, 437 MB in 96 us (4.6 TB/s; a large copy reaches
+// 5.1), 167 with eight wavefronts in one workgroup per unit.  One token behind 1000: 10.4 us, a chain of lengths, table entry, rows,
+// the tile, the partial results' way out, the counter and their way back.
 // ---------------------------------------------------------------------------------------
 constexpr int kManyQuantum = 64;
 
@@ -671,36 +675,42 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   // sixteen threads per row merge the wavefronts' partials
   const int rows = min(kPgRows, j.q.n * a.G - first_row);
   for (int r0 = 0; r0 < rows; r0 += kFewWaves * 4) {
-  const int row = r0 + (tid >> 4);
-  const PgOut to = pg_out<D>(a, j, first_row + row);
-  float m[kFewWaves], M = -INFINITY, l = 0.f;
+    const int row = r0 + (tid >> 4);
+    const PgOut to = pg_out<D>(a, j, first_row + row);
+    float m[kFewWaves], M = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int k = 0; k < kFewWaves; ++k) {
-    m[k] = s_m[k][row];
-    M = fmaxf(M, m[k]);
-  }
+    for (int k = 0; k < kFewWaves; ++k) {
+      m[k] = s_m[k][row];
+      M = fmaxf(M, m[k]);
+    }
 #pragma unroll
-  for (int k = 0; k < kFewWaves; ++k) {
-    m[k] = pg_weight(m[k], M);
-    l = m[k] == 0.f ? l : fmaf(m[k], s_l[k][row], l);
-  }
+    for (int k = 0; k < kFewWaves; ++k) {
+      m[k] = pg_weight(m[k], M);
+      l = m[k] == 0.f ? l : fmaf(m[k], s_l[k][row], l);
+    }
 #pragma unroll
-  for (int p = 0; p < D / 64; ++p) {
-    const int d = (tid & 15) * 4 + 64 * p;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < D / 64; ++p) {
+      const int d = (tid & 15) * 4 + 64 * p;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
-    if (j.parts == 1) pg_write_out(a, to, d, y, 1.f / l);
-    else if (row < rows) PgParts<D>::store(a, row, d, y);
-  }
-  if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D>::store_sums(a, row, M, l);
+      for (int k = 0; k < kFewWaves; ++k) pg_add4(y, m[k], *(const float4 *)((const float *)(s_tile + k * L::kBytes) + row * L::OROW + d));
+      if (j.parts == 1) pg_write_out(a, to, d, y, 1.f / l);
+      else if (row < rows) PgParts<D>::store(a, row, d, y);
+    }
+    if (j.parts > 1 && row < rows && (tid & 15) == 0) PgParts<D>::store_sums(a, row, M, l);
   }
   if (j.parts > 1) PgParts<D>::merge(a, j, (float *)s_tile);
   static_assert(PgParts<D>::kRoom * 4 <= sizeof(s_tile));
 }
 
 // ---------------------------------------------------------------------------------------
-// More rows: bound by the matrix products and the exponentials.  Four wavefronts of 32 * RB rows each share tiles of 64 keys.
+// More rows: bound by the matrix products and the exponentials, and in the end by power.  Eight wavefronts of 32 rows each share tiles
+// of 64 keys in three buffers, one barrier per tile; the tile after the next is on its way.
+// Four prompts of 8192 tokens (32 heads, 8 kv-heads, 128 channels): 2.25 ms, 980 TFLOP/s where a large library product reaches 1136.  The
+// matrix units are busy in 46 % of the cycles and the vector units in as many, at 1.73 of 2.4 GHz: whatever fills the cycles
+// better lowers the clock.  On the way: tiles through registers with padded rows 3.75 ms; straight into LDS 2.57; addresses of whole tiles
+// from scalars 2.51; scores a step ahead 2.46 (before: four wavefronts and two buffers, two workgroups to a unit).  64 rows a
+// wavefront, which halves the reads of the tiles, leave one wavefront to a SIMD: 2.9 to 3.0.
 //
 // Rows come straight into LDS (16 bytes a lane, no registers on the way), so a tile's rows lie as they are, 2 D bytes apart, and the
 // pieces of a row are permuted instead: piece p of row r lies at slot p ^ f(r), with an f that puts what the reads below take
@@ -852,7 +862,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   };
   int buffer = 0;
   auto next_buffer = [&](int b) { return b + 1 == kManyBuffers ? 0 : b + 1; };
-  auto turn = [&](int t, bool tail) {                    // tile t is there, and the next one but kBuffers - 2 is requested
+  auto turn = [&](int t, bool tail) {                    // tiles t and t + 1 are there, t + 2 is requested
     pg_arrive();
     if (tail) {
       scrub(t, buffer);
@@ -975,8 +985,8 @@ __global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a
 // ---------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------
-// Slots of a split call, by the rows of a block: a workgroup of many rows per compute unit; of few rows, whose sequences may be of any
-// length, some more, so that no part is much longer than the others.
+// Slots of a split call: as many as there are workgroups on the chip at a time, one of many rows to a compute unit or two of few (with
+// twice as many 8 tokens behind 2000 took 25.8 us instead of 20.9, 32 behind 600 27.3 instead of 24.0).
 constexpr int kManySlots = 256, kFewSlots = 512;
 constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
 size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
