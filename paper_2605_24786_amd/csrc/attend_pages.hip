@@ -79,7 +79,7 @@ struct PgJob {
 constexpr int kManyLeastPart = 256;
 template <int R, int QUANTUM>
 __device__ __forceinline__ unsigned pg_least_part(const PagesLaunch &a, unsigned longest) {
-  if constexpr (R != kPgRows) return (longest * QUANTUM < 2 * kManyLeastPart ? longest : kManyLeastPart / QUANTUM);
+  if constexpr (R != kPgRows) return longest * QUANTUM < 2 * kManyLeastPart ? longest : kManyLeastPart / QUANTUM;
   const float rows = (float)min((long long)a.tokens * a.G, (long long)R);
   return max(1u, (unsigned)(__builtin_sqrtf((float)longest * QUANTUM * rows * 1.9f) * (1.f / QUANTUM) + 0.5f));
 }
@@ -122,19 +122,21 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
   auto length = [](const PgSequence &q) { return (unsigned)(q.c + q.n + (QUANTUM - 1)) / QUANTUM; };   // in quanta
   unsigned part = 0;                                   // quanta of a part; 0: none is cut
   if (a.slots > 0) {
-    const unsigned most = (unsigned)a.slots / (unsigned)a.Hkv;   // (block, part) pairs per kv-head
-    int blocks = 0;
-    unsigned longest = 0;
-    float work = 0.f;
+    const unsigned most = (unsigned)a.slots_per_head;    // (block, part) pairs per kv-head
+    unsigned blocks = 0, longest = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
       const PgSequence q = sequence(b0);
-      const int n = blocks_of(q);
-      blocks += pg_last(pg_scan(n));
-      work += (float)pg_last(pg_scan((int)fminf((float)n * (float)length(q), 0x1p24f)));   // (an estimate to begin with)
+      blocks += (unsigned)pg_last(pg_scan(blocks_of(q)));
       longest = max(longest, (unsigned)pg_max((int)length(q)));
     }
-    if (blocks > 0 && (unsigned)blocks <= most) {
-      part = max(pg_least_part<R, QUANTUM>(a, longest), (unsigned)(work / (float)most));
+    const unsigned least = pg_least_part<R, QUANTUM>(a, longest);
+    if (blocks > 0 && blocks <= most && least < longest) {
+      float work = 0.f;                                  // (an estimate to begin with)
+      for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        const PgSequence q = sequence(b0);
+        work += (float)pg_last(pg_scan((int)fminf((float)blocks_of(q) * (float)length(q), 0x1p24f)));
+      }
+      part = max(least, (unsigned)(work / (float)most));
       for (;;) {
         unsigned jobs = 0;
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
@@ -146,18 +148,18 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
       }
     }
   }
-  j.g = x % (unsigned)a.Hkv;
-  int at = x / (unsigned)a.Hkv;
+  int at = a.h_magic ? (int)(__umulhi(x, a.h_magic) >> a.h_shift) : (int)x;   // x / Hkv
+  j.g = (int)(x - (unsigned)at * (unsigned)a.Hkv);
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const PgSequence q = sequence(b0);
     const int blocks = blocks_of(q), parts = part ? (int)((length(q) + part - 1) / part) : 1;
     const int jobs = blocks * parts;
     int end = pg_scan(jobs);
     const int all = pg_last(end);
-    if (R != kPgRows && a.B > 1 && a.B <= kWave) {
+    const int len = q.c + q.n;
+    if (R != kPgRows && a.B <= kWave && __builtin_amdgcn_ballot_w64(lane < a.B && len != __builtin_amdgcn_readlane(len, 0))) {
       // long sequences first: the workgroups that come last shall have little to do (16 sequences of 0 to 700 tokens behind up
-      // to 5000: 416 -> 330 us)
-      const int len = q.c + q.n;
+      // to 5000: 416 -> 393 us)
       end = jobs;
       for (int i = 0; i < a.B; ++i) {
         const int other = __builtin_amdgcn_readlane(len, i);
@@ -170,9 +172,9 @@ __device__ __forceinline__ bool pg_job(const PagesLaunch &a, unsigned x, PgJob &
       at -= __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(jobs, l);
       j.b = b0 + l;
       j.parts = __builtin_amdgcn_readlane(parts, l);
-      j.block = at / j.parts;
-      j.part = at - j.block * j.parts;
-      j.block = __builtin_amdgcn_readlane(blocks, l) - 1 - j.block;
+      const int back = j.parts > 1 ? at / j.parts : at;
+      j.part = at - back * j.parts;
+      j.block = __builtin_amdgcn_readlane(blocks, l) - 1 - back;
       j.part_keys = j.parts > 1 ? (int)(part * QUANTUM) : kNoSplit;
       j.q.n = __builtin_amdgcn_readlane(q.n, l);
       j.q.c = __builtin_amdgcn_readlane(q.c, l);
@@ -568,17 +570,27 @@ struct PgParts {
 // The new tokens whose first row lies in rows [lo, hi) of the sequence go to their pages (an entry that is no page: nowhere).
 template <int D>
 __device__ __forceinline__ void pg_append(const PagesLaunch &a, const PgJob &j, int lo, int hi, int threads) {
-  if (!a.knew || j.part != 0) return;
-  constexpr int PR = D / 8;
+  if (!a.knew || j.part != j.parts - 1) return;          // (the last part is the shortest)
+  constexpr int PR = D / 8, kAhead = 4;                  // pieces of a thread whose rows are requested together
   const int t0 = pg_token(a, lo + a.G - 1), t1 = min(j.q.n, pg_token(a, hi + a.G - 1));
-  for (int i = threadIdx.x; i < (t1 - t0) * PR; i += threads) {
-    const int t = t0 + i / PR, at = j.q.c + t;
-    const int e = a.pages.table[j.b * a.pages.table_stride + (at >> a.pages.lg)];
-    if ((unsigned)e >= (unsigned)a.pages.n_pages) continue;
-    const long long from = ((j.q.s + t) * (long long)a.Hkv + j.g) * D + i % PR * 8;
-    const long long to = a.pages.offset(e, at, j.g) + i % PR * 8;
-    *(int4 *)(a.pages.k + to) = *(const int4 *)(a.knew + from);
-    *(int4 *)(a.pages.v + to) = *(const int4 *)(a.vnew + from);
+  const int32_t *table = a.pages.table + j.b * a.pages.table_stride;
+  for (int i0 = threadIdx.x; i0 < (t1 - t0) * PR; i0 += kAhead * threads) {
+    pg_u4 k[kAhead], v[kAhead];
+    long long to[kAhead];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const int i = i0 + n * threads, t = min(t0 + i / PR, t1 - 1), at = j.q.c + t, e = table[at >> a.pages.lg];
+      const long long from = ((j.q.s + t) * (long long)a.Hkv + j.g) * D + i % PR * 8;
+      k[n] = *(const pg_u4 *)(a.knew + from);
+      v[n] = *(const pg_u4 *)(a.vnew + from);
+      to[n] = i < (t1 - t0) * PR && (unsigned)e < (unsigned)a.pages.n_pages ? a.pages.offset(e, at, j.g) + i % PR * 8 : -1;
+    }
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      if (to[n] < 0) continue;
+      *(pg_u4 *)(a.pages.k + to[n]) = k[n];
+      *(pg_u4 *)(a.pages.v + to[n]) = v[n];
+    }
   }
 }
 
@@ -631,6 +643,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     ent = src.entry(key0 + kFewQuantum + l32);
   }
   st.init(a, j, first_row);
+  pg_append<D>(a, j, first_row, first_row + kPgRows, kFewWaves * kWave);
   const int end = min(hi, st.most);
   const float c = a.sm_scale * 1.44269504088896341f;
   uint8_t *Kt = s_tile + w * L::kBytes, *Vt = Kt + kPgKeys * L::KROW;
@@ -670,7 +683,6 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     s_l[w][l32] = sum;
   }
   st.template store_partial<L::OROW>((float *)(s_tile + w * L::kBytes) + l32 * L::OROW);
-  pg_append<D>(a, j, first_row, first_row + kPgRows, kFewWaves * kWave);
   __syncthreads();
   // sixteen threads per row merge the wavefronts' partials
   const int rows = min(kPgRows, j.q.n * a.G - first_row);
@@ -844,6 +856,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   M st;
   st.init(a, j, first_row);
   issue(1, 1);
+  pg_append<D>(a, j, first_row, first_row + R, kManyThreads);   // (its trip to memory beside that of the first tiles)
   __syncthreads();
   bool dropped = false;
   // Values of keys that some row does not see meet it with probability 0, which does not silence an infinite or NaN one: where
@@ -912,17 +925,16 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
     }
   }
   __syncthreads();
-  pg_append<D>(a, j, first_row, first_row + R, kManyThreads);
   // the wavefront's rows through LDS, 64 channels at a time in its own share of the tiles' room, so that they leave as whole lines
   float *wo = (float *)s_tile + w * kPgRows * 64;
   const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l);
-  const int l32 = lane & 31, h = lane >> 5;
-  PgOut to[kPgRows / 4];
-  float inv[kPgRows / 4];
+  const int l32 = lane & 31, h = lane >> 5, r8 = lane >> 3, c8 = lane & 7;   // a row of 64 channels to eight lanes
+  PgOut to[kPgRows / 8];
+  float inv[kPgRows / 8];
 #pragma unroll
-  for (int p = 0; p < kPgRows / 4; ++p) {
-    to[p] = pg_out<D>(a, j, first_row + w * kPgRows + 4 * p + (lane >> 4));
-    inv[p] = 1.f / __shfl(l, 4 * p + (lane >> 4), kWave);
+  for (int p = 0; p < kPgRows / 8; ++p) {
+    to[p] = pg_out<D>(a, j, first_row + w * kPgRows + 8 * p + r8);
+    inv[p] = 1.f / __shfl(l, 8 * p + r8, kWave);
   }
 #pragma unroll
   for (int q = 0; q < D / 64; ++q) {
@@ -935,11 +947,24 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
       }
     pg_wave_sync();
 #pragma unroll
-    for (int p = 0; p < kPgRows / 4; ++p) {
-      const int r = 4 * p + (lane >> 4), row = w * kPgRows + r, d = (lane & 15) * 4 + 64 * q;
-      const float4 y = *(const float4 *)(wo + r * 64 + (((lane & 15) ^ (r & 15)) << 2));
-      if (j.parts == 1) pg_write_out(a, to[p], d, y, inv[p]);
-      else if (first_row + row <= last_row) *(float4 *)(a.o + ((long long)blockIdx.x * R + row) * D + d) = y;
+    for (int p = 0; p < kPgRows / 8; ++p) {
+      const int r = 8 * p + r8, row = w * kPgRows + r, d = c8 * 8 + 64 * q;
+      const float4 y0 = *(const float4 *)(wo + r * 64 + (((2 * c8) ^ (r & 15)) << 2)), y1 = *(const float4 *)(wo + r * 64 + (((2 * c8 + 1) ^ (r & 15)) << 2));
+      if (j.parts == 1) {
+        float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+        pg_h8 out;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] *= inv[p];
+          if (a.lambda) y[e] = fmaf(-to[p].f, __shfl_xor(y[e], 8, kWave), y[e]);   // (the pair's other row, in the next eight lanes)
+          out[e] = (_Float16)y[e];
+        }
+        if (to[p].at) *(pg_h8 *)(to[p].at + d) = out;
+      } else if (first_row + row <= last_row) {
+        float4 *o = (float4 *)(a.o + ((long long)blockIdx.x * R + row) * D + d);
+        o[0] = y0;
+        o[1] = y1;
+      }
     }
     pg_wave_sync();
   }
@@ -1000,6 +1025,7 @@ static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, int threa
   const long long most = a.Hkv * std::min(a.B * each, (long long)a.rows * a.G / R + a.B);
   const bool may_split = scratch && (long long)a.pages.max_pages << a.pages.lg > least_part && (a.count || a.B * each * a.Hkv <= slots);
   a.slots = may_split ? slots : 0;
+  a.slots_per_head = a.slots / a.Hkv;
   a.ml = (float2 *)scratch;
   a.o = scratch + kSlotRows * 2;
   const long long grid = std::max<long long>(most, a.slots);
@@ -1009,6 +1035,7 @@ template <int D>
 static hipError_t launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
   const bool few = (long long)a.tokens * a.G <= kPgRows;
   a.g_magic = a.G > 1 ? split_divisor(a.G, &a.g_shift) : 0u;
+  a.h_magic = a.Hkv > 1 ? split_divisor(a.Hkv, &a.h_shift) : 0u;
   const unsigned grid = few ? plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, kFewWaves * kWave, scratch)
                             : plan_blocks<kManyRows>(a, kManySlots, 2 * kManyLeastPart - kManyKeys, kManyThreads, scratch);
   if (grid == 0) return hipErrorInvalidValue;

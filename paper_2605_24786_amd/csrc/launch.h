@@ -116,7 +116,7 @@ struct AttendLaunch {
 enum AttendKind { kAttendPlain, kAttendShared, kAttendDiff };
 constexpr int kAttendMaxSplits = 64;
 constexpr int kChunkRows = 16;     // query rows per unit of a multi-token call (one matrix-core tile)
-// Multiplier and shift of a division by ns (2 .. 64): x / ns = (high word of x * multiplier) >> shift for all 0 <= x < 2^31.
+// Multiplier and shift of a division by ns >= 2: x / ns = (high word of x * multiplier) >> shift for all 0 <= x < 2^31.
 unsigned split_divisor(int ns, int *shift);
 bool attend_supported(int D, int G);
 size_t attend_spill_floats(int units_per_layer, int G, int cap);   // scratch the two-launch form needs
@@ -167,10 +167,10 @@ struct PagesLaunch {
   const float *lambda;                     // null, or weights [rows][Hkv * G / 2], rows lambda_stride apart
   long long lambda_stride;
   int B, Hkv, G;
-  unsigned g_magic;                        // a division by G (split_divisor), 0 for 1; filled in by the launcher, as all below
-  int g_shift;
+  unsigned g_magic, h_magic;               // divisions by G and Hkv (split_divisor), 0 for 1; filled in by the launcher, as all below
+  int g_shift, h_shift;
   float sm_scale;
-  int slots;                               // (block, part) pairs of a split call at most
+  int slots, slots_per_head;               // (block, part) pairs of a split call at most
   float2 *ml;
   float *o;
   unsigned *arrived;                       // [kPagesCounters], zero between calls: parts of a block that have left their results
