@@ -307,8 +307,9 @@ class ConfKV:
                 pages_v.dtype is half and pages_v.shape == shape and pages_v.stride() == apart and pages_k.get_device() == device and
                 pages_v.get_device() == device and len(rows) == 2 and rows[0] == B and table.dtype is self._i32 and
                 table.get_device() == device and (step[1] == 1 or rows[1] == 1)):
-            return _PAGES.pack(pages_k.data_ptr(), pages_v.data_ptr(), apart[0], apart[1], apart[2], shape[1], shape[0], table.data_ptr(),
-                               step[0] if B > 1 else rows[1], rows[1])
+            # (a size of 1 may come with any stride)
+            return _PAGES.pack(pages_k.data_ptr(), pages_v.data_ptr(), apart[0] if shape[0] > 1 else 0, apart[1],
+                               apart[2] if shape[2] > 1 else 0, shape[1], shape[0], table.data_ptr(), step[0] if B > 1 else rows[1], rows[1])
         raise ValueError(f"pages_k, pages_v: float16 [pages][page][{self._kv_heads}][{self._head_dim}] with dense heads and equal strides, and "
                          f"table: int32 [{B}][pages per sequence] with dense rows, on {self.state.device} are wanted, got {pages_k.dtype} "
                          f"{tuple(shape)} {apart}, {pages_v.dtype} {tuple(pages_v.shape)} {pages_v.stride()}, {table.dtype} {tuple(rows)} "

@@ -189,6 +189,48 @@ def test_large_scores(lib, torch_cuda):
     _Case(lib, torch_cuda, 128, 4, 1, 16, [2], [900], spread=12.0).run()
 
 
+def test_calls_without_new_tokens(lib, torch_cuda):
+    """Nobody has any, no rows, no tokens: nothing is written."""
+    for n in (0, 3):
+        c = _Case(lib, torch_cuda, 128, 4, 2, 16, [n, 0], [30, 7])
+        c.new = [0, 0]
+        before = [p.clone() for p in c.pages]
+        for tokens in (1, 3, 50, 0):
+            c.call(tokens=tokens)
+            assert (c.out == c.MARK).all()
+        assert all(torch_cuda.equal(a.view(torch_cuda.int16), b.view(torch_cuda.int16)) for a, b in zip(before, c.pages))
+        c.kv.close()
+    kv = _handle(lib, 1, 4, 2, 128, 64)
+    t = lambda *s: torch_cuda.zeros(s, dtype=torch_cuda.float16, device="cuda")
+    i32 = torch_cuda.zeros(1, dtype=torch_cuda.int32, device="cuda")
+    kv.attend_pages(t(0, 8, 128), t(0, 2, 128), t(0, 2, 128), t(0, 8, 128), t(4, 16, 2, 128), t(4, 16, 2, 128), i32.reshape(1, 1), i32, tokens=4,
+                    starts=i32)
+    kv.close()
+
+
+@pytest.mark.parametrize("T", [1, 30])
+def test_rows_of_padded_batches(lib, torch_cuda, T):
+    """[B][T] rows of which every sequence uses its first ones; weights for all rows at once; one kv-head, one page."""
+    torch, B, wide = torch_cuda, 3, T + 2
+    new = [T, max(0, T - 1), min(T, 2)]
+    c = _Case(lib, torch, 128, 2, 1, 64, new, [3, 0, 60 - T], diff=True, gap=0)
+    q, k, v = (np.full((B, wide) + x.shape[1:], 9.0, np.float16) for x in (c.q, c.k[0], c.v[0]))
+    for b, (n, s) in enumerate(zip(new, c.starts)):
+        q[b, :n], k[b, :n], v[b, :n] = c.q[s:s + n], c.k[b][c.context[b]:], c.v[b][c.context[b]:]
+    c.lam = np.broadcast_to(c.lam[0], c.lam.shape)
+    out = torch.full((B, wide, 1, 128), c.MARK, dtype=torch.float16, device="cuda")
+    i32 = lambda x: c.on(np.array(x, np.int32))
+    pages = [p.as_strided(p.shape, (p.stride(0), p.stride(1), 1, 1)) for p in c.pages]        # (a stride that nothing uses)
+    c.kv.attend_pages(c.on(q), c.on(k), c.on(v), out, *pages, c.on(c.table), i32(c.context), tokens=T, starts=i32([b * wide for b in range(B)]),
+                      new=i32(new), lam=c.on(c.lam[0]))
+    c.out = torch.full((c.R, 1, 128), c.MARK, dtype=torch.float16, device="cuda")
+    for b, (n, s) in enumerate(zip(new, c.starts)):
+        c.out[s:s + n] = out[b, :n]
+        assert (out[b, n:] == c.MARK).all()
+    c.check()
+    c.kv.close()
+
+
 def test_more_than_a_wavefront_of_sequences(lib, torch_cuda):
     B = 150
     _Case(lib, torch_cuda, 64, 2, 1, 8, [(1, 0, 2)[b % 3] for b in range(B)], [b % 40 for b in range(B)], gap=0).run()
