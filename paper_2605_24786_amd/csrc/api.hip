@@ -367,7 +367,7 @@ static bool pages_ok(const conf_kv_handle *h, const conf_kv_pages &p) {
   if ((((uintptr_t)p.dev_k16 | (uintptr_t)p.dev_v16) & 15) || ((uintptr_t)p.dev_table & 3)) return false;
   if (p.page_tokens < 8 || p.page_tokens > 1 << 20 || (p.page_tokens & (p.page_tokens - 1))) return false;
   if (p.n_pages < 1 || p.n_pages > 1 << 30 || p.max_pages < 1 || (long long)p.max_pages * p.page_tokens > 1ll << 30) return false;
-  if (p.table_stride < p.max_pages || p.table_stride > (int64_t)1 << 40) return false;
+  if (p.table_stride < p.max_pages || p.table_stride > ((int64_t)1 << 56) / h->cfg.batch) return false;
   return pages_extent(h, p) > 0;
 }
 static PagesView pages_view(const conf_kv_pages &p) {
@@ -432,7 +432,7 @@ int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const co
   if (!c.dev_context || !c.dev_q16 || !c.dev_out16 || !c.dev_knew16 != !c.dev_vnew16) return CONF_KV_ERR_INVALID_ARG;
   if (((uintptr_t)c.dev_q16 | (uintptr_t)c.dev_knew16 | (uintptr_t)c.dev_vnew16 | (uintptr_t)c.dev_out16) & 15) return CONF_KV_ERR_INVALID_ARG;
   if (((uintptr_t)c.dev_starts | (uintptr_t)c.dev_new | (uintptr_t)c.dev_context | (uintptr_t)c.dev_lambda) & 3) return CONF_KV_ERR_INVALID_ARG;
-  if (c.dev_lambda && (G % 2 || c.lambda_stride < 0 || c.lambda_stride > (int64_t)1 << 40)) return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_lambda && (G % 2 || c.lambda_stride < 0 || c.lambda_stride > ((int64_t)1 << 56) / c.rows)) return CONF_KV_ERR_INVALID_ARG;
   const size_t q_bytes = (size_t)c.rows * Hq * D * 2, new_bytes = (size_t)c.rows * H * D * 2, out_bytes = c.dev_lambda ? q_bytes / 2 : q_bytes;
   const size_t page_bytes = (size_t)pages_extent(h, *pages) * 2;
   if (overlap(c.dev_out16, out_bytes, c.dev_q16, q_bytes)) return CONF_KV_ERR_INVALID_ARG;
@@ -442,6 +442,15 @@ int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const co
       if (fresh && (overlap(fresh, new_bytes, plane, page_bytes) || overlap(fresh, new_bytes, c.dev_out16, out_bytes))) return CONF_KV_ERR_INVALID_ARG;
     if (c.dev_knew16 && overlap(c.dev_q16, q_bytes, plane, page_bytes)) return CONF_KV_ERR_INVALID_ARG;
   }
+  if (c.dev_knew16 && pages->dev_k16 == pages->dev_v16) return CONF_KV_ERR_INVALID_ARG;
+  const struct { const void *at; size_t bytes; } read[] = {                       // what tells the rows and their weights apart
+      {c.dev_starts, (size_t)B * 4}, {c.dev_new, (size_t)B * 4}, {c.dev_context, (size_t)B * 4},
+      {pages->dev_table, ((size_t)(B - 1) * pages->table_stride + pages->max_pages) * 4},
+      {c.dev_lambda, ((size_t)(c.rows - 1) * c.lambda_stride + Hq / 2) * 4}};
+  for (const auto &r : read)
+    if (r.at && (overlap(r.at, r.bytes, c.dev_out16, out_bytes) ||
+                 (c.dev_knew16 && (overlap(r.at, r.bytes, pages->dev_k16, page_bytes) || overlap(r.at, r.bytes, pages->dev_v16, page_bytes)))))
+      return CONF_KV_ERR_INVALID_ARG;
   if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
   PagesLaunch a{};
   a.pages = pages_view(*pages);

@@ -423,6 +423,20 @@ def test_refusals(lib, torch_cuda):
     assert status(table=t(B, 5, d=i32)) == b.ERR_INVALID_ARG                       # more than max_paged
     assert status(knew16=None) == b.ERR_INVALID_ARG
     assert status(out16=ok["q16"]) == b.ERR_INVALID_ARG
+    # Tensors that are read and written: the same keys and values, lengths and tables inside the outputs or the pages.
+    assert status(pages_v=ok["pages_k"]) == b.ERR_INVALID_ARG
+    kv.attend_pages(**dict(ok, pages_v=ok["pages_k"], knew16=None, vnew16=None))
+    for place in ("out16", "pages_v"):
+        ints = ok[place].view(i32).reshape(-1)
+        for name in ("starts", "new", "context"):
+            assert status(**{name: ints[1:3]}) == b.ERR_INVALID_ARG
+        assert status(table=ints[:8].reshape(2, 4)) == b.ERR_INVALID_ARG
+    pairs = _handle(lib, B, 2, H, D, 4 * page)
+    for place in ("out", "pages_v"):
+        out = t(B, 2, 2, D)
+        with pytest.raises(lib.ConfKVError):
+            pairs.attend_pages(**dict(ok, q16=t(B, 2, 4, D), out16=out, lam=(out if place == "out" else ok[place]).view(torch.float32).reshape(-1)[2:4]))
+    pairs.close()
     for bad in (12, 4):
         assert status(pages_k=t(9, bad, H, D), pages_v=t(9, bad, H, D)) == b.ERR_INVALID_ARG
     once = t(1, page, H, D).expand(9, page, H, D)
