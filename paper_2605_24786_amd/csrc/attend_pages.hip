@@ -32,6 +32,10 @@ __device__ __forceinline__ pg_h4 pg_read_tr(const uint8_t *p) {
   return __builtin_bit_cast(pg_h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pg_s4 *)p));
 }
 __device__ __forceinline__ float pg_other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// Of lanes 2 i and 2 i + 1, the other's.
+__device__ __forceinline__ float pg_neighbour(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));   // quad_perm:[1,0,3,2]
+}
 // The signs of the result: which of two halfs are infinite or NaN (their magnitude, 0x7c00 or more, carries into the sign).
 typedef unsigned pg_u4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ pg_u4 pg_odd_halfs(pg_u4 d) { return ((d & 0x7fff7fffu) + 0x04000400u) & 0x80008000u; }
@@ -579,6 +583,8 @@ __device__ __forceinline__ void pg_append(const PagesLaunch &a, const PgJob &j, 
     long long to[kAhead];
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) {
+      to[n] = -1;
+      if (__builtin_amdgcn_readfirstlane(i0) + n * threads >= (t1 - t0) * PR) continue;
       const int i = i0 + n * threads, t = min(t0 + i / PR, t1 - 1), at = j.q.c + t, e = table[at >> a.pages.lg];
       const long long from = ((j.q.s + t) * (long long)a.Hkv + j.g) * D + i % PR * 8;
       k[n] = *(const pg_u4 *)(a.knew + from);
@@ -877,6 +883,9 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   auto next_buffer = [&](int b) { return b + 1 == kManyBuffers ? 0 : b + 1; };
   auto turn = [&](int t, bool tail) {                    // tiles t and t + 1 are there, t + 2 is requested
     pg_arrive();
+    // The entries among it, which the compiler learns here: it waited for them in front of the next ones' request otherwise, and so for
+    // the tile just requested (15 % of the loop, where registers happened to fall that way).
+    asm volatile("" : "+v"(ent));
     if (tail) {
       scrub(t, buffer);
       pg_arrive();
@@ -925,50 +934,68 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
     }
   }
   __syncthreads();
-  // the wavefront's rows through LDS, 64 channels at a time in its own share of the tiles' room, so that they leave as whole lines
-  float *wo = (float *)s_tile + w * kPgRows * 64;
   const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l);
-  const int l32 = lane & 31, h = lane >> 5, r8 = lane >> 3, c8 = lane & 7;   // a row of 64 channels to eight lanes
-  PgOut to[kPgRows / 8];
-  float inv[kPgRows / 8];
+  const int l32 = lane & 31, h = lane >> 5, row0 = w * kPgRows;
+  if (j.parts > 1) {
+    // the wavefront's rows through LDS, 64 channels at a time in its own share of the tiles' room, so that they leave as whole lines
+    float *wo = (float *)s_tile + row0 * 64;
 #pragma unroll
-  for (int p = 0; p < kPgRows / 8; ++p) {
-    to[p] = pg_out<D>(a, j, first_row + w * kPgRows + 8 * p + r8);
-    inv[p] = 1.f / __shfl(l, 8 * p + r8, kWave);
-  }
+    for (int q = 0; q < D / 64; ++q) {
 #pragma unroll
-  for (int q = 0; q < D / 64; ++q) {
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {                      // (sixteen bytes to the place that keeps rows on different banks)
-        const pg_f16 &o = st.rows.O[2 * q + nt];
-        *(float4 *)(wo + l32 * 64 + (((8 * nt + 2 * i + h) ^ (l32 & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      for (int i = 0; i < 8; ++i) {                      // (sixteen bytes to the place that keeps rows on different banks)
+        const pg_f16 &o = st.rows.O[2 * q + i / 4];
+        const int e = i % 4 * 4;
+        *(float4 *)(wo + l32 * 64 + (((2 * i + h) ^ (l32 & 15)) << 2)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
-    pg_wave_sync();
+      pg_wave_sync();
 #pragma unroll
-    for (int p = 0; p < kPgRows / 8; ++p) {
-      const int r = 8 * p + r8, row = w * kPgRows + r, d = c8 * 8 + 64 * q;
-      const float4 y0 = *(const float4 *)(wo + r * 64 + (((2 * c8) ^ (r & 15)) << 2)), y1 = *(const float4 *)(wo + r * 64 + (((2 * c8 + 1) ^ (r & 15)) << 2));
-      if (j.parts == 1) {
-        float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-        pg_h8 out;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          y[e] *= inv[p];
-          if (a.lambda) y[e] = fmaf(-to[p].f, __shfl_xor(y[e], 8, kWave), y[e]);   // (the pair's other row, in the next eight lanes)
-          out[e] = (_Float16)y[e];
-        }
-        if (to[p].at) *(pg_h8 *)(to[p].at + d) = out;
-      } else if (first_row + row <= last_row) {
-        float4 *o = (float4 *)(a.o + ((long long)blockIdx.x * R + row) * D + d);
-        o[0] = y0;
-        o[1] = y1;
+      for (int p = 0; p < kPgRows / 4; ++p) {
+        const int r = 4 * p + (lane >> 4), piece = lane & 15;
+        const float4 y = *(const float4 *)(wo + r * 64 + ((piece ^ (r & 15)) << 2));
+        if (first_row + row0 + r <= last_row) *(float4 *)(a.o + ((long long)blockIdx.x * R + row0 + r) * D + 64 * q + 4 * piece) = y;
       }
+      pg_wave_sync();
     }
-    pg_wave_sync();
+    if (lane < kPgRows) a.ml[(long long)blockIdx.x * R + row0 + lane] = make_float2(m, l);
+    return;
   }
-  if (j.parts > 1 && lane < kPgRows) a.ml[(long long)blockIdx.x * R + w * kPgRows + lane] = make_float2(m, l);
+  // The same in fp16.  Instructions count here, and a division or a wide product per row costs four to ten: rows are counted from the
+  // block's first token (fewer than 256 + G; G is at most 16, so that the product with 65536 / G + 1 divides exactly).
+  const int first_token = pg_token(a, first_row), ahead = first_row - first_token * a.G;
+  auto token = [&](int rel) { return (int)(__umul24(rel, a.g_mul) >> 16); };
+  const int heads = a.lambda ? a.G >> 1 : a.G;           // of the output
+  float f = 0.f;
+  if (a.lambda) {
+    const int rel = ahead + min(row0 + l32, last_row - first_row), t = token(rel);
+    f = a.lambda[(long long)(j.q.s + first_token + t) * a.lambda_stride + j.g * heads + ((rel - t * a.G) >> 1)];
+  }
+  const float inv = 1.f / l;
+  uint8_t *wo = s_tile + row0 * 2 * D;
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    const pg_f16 &o = st.rows.O[i / 4];
+    pg_h4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float y = o[i % 4 * 4 + e] * inv;
+      if (a.lambda) y = fmaf(-f, pg_neighbour(y), y);    // (the pair's other row)
+      out[e] = (_Float16)y;
+    }
+    *(pg_h4 *)(wo + l32 * 2 * D + ((i ^ (l32 % PR)) << 4) + 8 * h) = out;
+  }
+  pg_wave_sync();
+  __half *base = a.out + ((long long)(j.q.s + first_token) * a.Hkv + j.g) * heads * D;
+#pragma unroll
+  for (int p = 0; p < kPgRows / 8; ++p) {                // eight rows, 64 channels of them at a time
+    const int r = 8 * p + (lane >> 3), rel = ahead + row0 + r, t = token(rel), hq = rel - t * a.G;
+    __half *to = base + ((long long)t * (a.Hkv * heads) + (a.lambda ? hq >> 1 : hq)) * D + (lane & 7) * 8;
+    const bool leaves = first_row + row0 + r <= last_row && !(a.lambda && (hq & 1));
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) {
+      const pg_h8 out = *(const pg_h8 *)(wo + r * 2 * D + (((8 * q + (lane & 7)) ^ (r % PR)) << 4));
+      if (leaves) *(pg_h8 *)(to + 64 * q) = out;
+    }
+  }
 }
 
 // Many rows: their parts' partial results are merged in a launch of its own, by as many workgroups as there are parts: alone, a
@@ -1034,6 +1061,7 @@ static unsigned plan_blocks(PagesLaunch &a, int slots, int least_part, int threa
 template <int D>
 static hipError_t launch_pages_of(PagesLaunch a, float *scratch, hipStream_t stream) {
   const bool few = (long long)a.tokens * a.G <= kPgRows;
+  a.g_mul = 65536 / a.G + 1;
   a.g_magic = a.G > 1 ? split_divisor(a.G, &a.g_shift) : 0u;
   a.h_magic = a.Hkv > 1 ? split_divisor(a.Hkv, &a.h_shift) : 0u;
   const unsigned grid = few ? plan_blocks<kPgRows>(a, kFewSlots, kFewQuantum, kFewWaves * kWave, scratch)

@@ -169,6 +169,7 @@ struct PagesLaunch {
   int B, Hkv, G;
   unsigned g_magic, h_magic;               // divisions by G and Hkv (split_divisor), 0 for 1; filled in by the launcher, as all below
   int g_shift, h_shift;
+  int g_mul;                               // 65536 / G + 1
   float sm_scale;
   int slots, slots_per_head;               // (block, part) pairs of a split call at most
   float2 *ml;
