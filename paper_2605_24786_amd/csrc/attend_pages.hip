@@ -724,11 +724,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 // ---------------------------------------------------------------------------------------
 // More rows: bound by the matrix products and the exponentials, and in the end by power.  Eight wavefronts of 32 rows each share tiles
 // of 64 keys in three buffers, one barrier per tile; the tile after the next is on its way.
-// Four prompts of 8192 tokens (32 heads, 8 kv-heads, 128 channels): 2.25 ms, 980 TFLOP/s where a large library product reaches 1136.  The
-// matrix units are busy in 46 % of the cycles and the vector units in as many, at 1.73 of 2.4 GHz: whatever fills the cycles
-// better lowers the clock.  On the way: tiles through registers with padded rows 3.75 ms; straight into LDS 2.57; addresses of whole tiles
-// from scalars 2.51; scores a step ahead 2.46 (before: four wavefronts and two buffers, two workgroups to a unit).  64 rows a
-// wavefront, which halves the reads of the tiles, leave one wavefront to a SIMD: 2.9 to 3.0.
+// Four prompts of 8192 tokens (32 heads, 8 kv-heads, 128 channels): 2.20 ms, 1000 TFLOP/s where a large library product reaches 1136.  The
+// matrix units are busy in 48 % of the cycles and the vector units in 47 %, at 1.68 of 2.4 GHz.  On the way: tiles through registers
+// with padded rows 3.75 ms; straight into LDS 2.57; addresses of whole tiles from scalars 2.51; scores a step ahead 2.46 (before: four
+// wavefronts and two buffers, two workgroups to a unit).  64 rows a wavefront, which halves the reads of the tiles, leave one wavefront
+// to a SIMD: 2.9 to 3.0, with their halves half a step apart 2.47.
 //
 // Rows come straight into LDS (16 bytes a lane, no registers on the way), so a tile's rows lie as they are, 2 D bytes apart, and the
 // pieces of a row are permuted instead: piece p of row r lies at slot p ^ f(r), with an f that puts what the reads below take
