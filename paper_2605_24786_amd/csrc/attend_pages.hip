@@ -253,13 +253,17 @@ template <int D>
 struct PgRows {
   pg_h8 qf[D / 16];
   pg_f16 O[D / 32];
-  // Probabilities are 2^(score * c + off): off follows the row's maximum, and lifts it to 2^10, so that as fp16 operands they keep
+  // Probabilities are 2^((score - ref) * c + off): off follows the row's maximum, and lifts it to 2^10, so that as fp16 operands they keep
   // eleven bits down to 2^-24 of the largest (unlifted 2^-14).  One fused operation per score, whose product is not rounded;
-  // what off is rounded to is off for all keys alike.
-  float off, l;
+  // what off is rounded to is off for all keys alike.  Up to kFar ref is 0.  Beyond, off's steps come near the slack that fp16
+  // leaves (2^27: 16 powers of two), so there the maximum is ref, taken away before the score is scaled, in a pass of its own
+  // that only wavefronts with such a row run (`far`).
+  float off, ref, limit, l;                            // limit: the score beyond which the reference moves
+  bool far;
   int row, lim, least, most;                           // row of the block; keys the lane's row sees; the fewest and the most
 
   static constexpr float kLift = 10.f, kSlack = 5.5f;  // 2^15.5 is 46341 of fp16's 65504
+  static constexpr float kFar = 0x1p20f;               // off within 2^-3 of what it is meant to be
 
   __device__ __forceinline__ void reset() {
 #pragma unroll
@@ -267,6 +271,9 @@ struct PgRows {
 #pragma unroll
       for (int i = 0; i < 16; ++i) O[nt][i] = 0.f;
     off = INFINITY;
+    ref = 0.f;
+    limit = -INFINITY;
+    far = false;
     l = 0.f;
   }
   // rows first .. first + 31 of the sequence's n * G
@@ -310,18 +317,29 @@ struct PgRows {
     return mx;
   }
   // The reference only has to stay near the maximum (the merges are exact for any), so the exchange and the rescaling run
-  // where a score passes it by more than kSlack.
-  __device__ __forceinline__ bool passes(float mx, float c) const { return fmaf(mx, c, off) > kLift + kSlack; }
+  // where a score passes it by more than kSlack (a far one at all: its steps are as long).
+  __device__ __forceinline__ bool passes(float mx) const { return mx > limit; }
   __device__ __forceinline__ void raise(float mx, float c) {
-    const float top = fmaxf(mx, pg_other_half(mx)) * c;
-    const float now = fminf(off, kLift - top);         // (no score yet: top is -inf and off stays)
-    const float corr = off == now ? 1.f : __builtin_amdgcn_exp2f(now - off);
+    const float top = fmaxf(mx, pg_other_half(mx)), scaled = top * c;
+    const bool higher = fmaf(top - ref, c, off) > kLift, distant = !(fabsf(scaled) < kFar);   // (no score yet: top is -inf, nothing is higher)
+    const float now_ref = !higher ? ref : distant ? top : 0.f, now = !higher ? off : distant ? kLift : kLift - scaled;
+    const float corr = higher ? __builtin_amdgcn_exp2f(fmaf(ref - now_ref, c, now - off)) : 1.f;
     off = now;
+    ref = now_ref;
+    limit = !higher ? limit : distant ? top : top + kSlack / c;
+    far = __builtin_amdgcn_ballot_w64(ref != 0.f) != 0ull;
     l *= corr;
 #pragma unroll
     for (int nt = 0; nt < D / 32; ++nt) O[nt] *= corr;
   }
-  // scores -> probabilities
+  __device__ __forceinline__ void follow(float mx, float c, pg_f16 &sc) {
+    if (__builtin_amdgcn_ballot_w64(passes(mx))) raise(mx, c);
+    if (__builtin_expect(far, 0)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] -= ref;
+    }
+  }
+  // scores, behind follow() -> probabilities
   __device__ __forceinline__ void weights(const pg_f16 &sc, float c, pg_h8 (&pb)[2]) {
     const float at = off == INFINITY ? 0.f : off;
     float sum[4];
@@ -337,7 +355,7 @@ struct PgRows {
   template <bool kMask>
   __device__ __forceinline__ void weigh(pg_f16 &sc, int key0, float c, pg_h8 (&pb)[2]) {
     const float mx = peak<kMask>(sc, key0);
-    if (__builtin_amdgcn_ballot_w64(passes(mx, c))) raise(mx, c);
+    follow(mx, c, sc);
     weights(sc, c, pb);
   }
   template <int VROW>
@@ -371,7 +389,7 @@ struct PgRows {
   }
   // Its maximum for the merges.  (No key: -inf.  A sum that is NaN, from a score that is none, outweighs the others: a merge shall not
   // lose it.)
-  __device__ __forceinline__ float maximum(float sum) const { return sum == sum ? -off : INFINITY; }
+  __device__ __forceinline__ float maximum(float sum, float c) const { return sum == sum ? fmaf(ref, c, -off) : INFINITY; }
   template <int OROW>
   __device__ __forceinline__ void store_partial(float *to) const {
     const int h = (threadIdx.x & 63) >> 5;
@@ -685,7 +703,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   const float sum = st.finish(src, lo, hi, dropped);
   // (no key: -inf stays; a sum that is NaN, from a score that is none, outweighs the others: a merge shall not lose it)
   if (h == 0) {
-    s_m[w][l32] = st.maximum(sum);
+    s_m[w][l32] = st.maximum(sum, c);
     s_l[w][l32] = sum;
   }
   st.template store_partial<L::OROW>((float *)(s_tile + w * L::kBytes) + l32 * L::OROW);
@@ -898,9 +916,9 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
   // these meet the values: matrix products beside vector arithmetic in either half of a step.
   pg_f16 sc[2];
   float mx = 0.f;
-  auto step = [&](int at, int next, const pg_f16 &now, pg_f16 &then) {
+  auto step = [&](int at, int next, pg_f16 &now, pg_f16 &then) {
     pg_h8 pb[2];
-    if (__builtin_amdgcn_ballot_w64(st.rows.passes(mx, st.c))) st.rows.raise(mx, st.c);
+    st.rows.follow(mx, st.c, now);
     __builtin_amdgcn_sched_barrier(0);
     st.scores(s_tile, next, then);
     st.rows.weights(now, st.c, pb);
@@ -934,7 +952,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(D 
     }
   }
   __syncthreads();
-  const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l);
+  const float l = st.rows.finish(src, lo, hi, dropped), m = st.rows.maximum(l, st.c);
   const int l32 = lane & 31, h = lane >> 5, row0 = w * kPgRows;
   if (j.parts > 1) {
     // the wavefront's rows through LDS, 64 channels at a time in its own share of the tiles' room, so that they leave as whole lines
