@@ -315,7 +315,8 @@ int conf_kv_attend_shared(conf_kv_handle *h, int32_t layer, int32_t tq, const co
  * one rounding at its end; importance is the size of the weight that a slot's value had, A_i = sum_j |w_i| (of one query; queries
  * of a call as in conf_kv_attend_chunk).  Tensors, errors and rules of conf_kv_attend_chunk (tq = 1: of conf_kv_attend) but for dev_out16,
  * fp16 [B][tq][Hq / 2][D], and dev_lambda, fp32 [B][tq][Hq / 2] with sequences batch_stride and tokens token_stride values apart
- * (0: the same weights for all).  An odd group or tq * n_q_heads / n_kv_heads above 16 is CONF_KV_ERR_INVALID_ARG.
+ * (0: the same weights for all).  An odd group, tq * n_q_heads / n_kv_heads above 16 and an output that overlaps what is read are
+ * CONF_KV_ERR_INVALID_ARG.
  * conf_kv_observe* see single maps: the importance they give sums to G per query, more than a step's here. */
 int conf_kv_attend_diff(conf_kv_handle *h, int32_t layer, int32_t tq, const float *dev_lambda, int64_t batch_stride,
                         int64_t token_stride, const void *dev_q16, const void *dev_knew16, const void *dev_vnew16, void *dev_out16,

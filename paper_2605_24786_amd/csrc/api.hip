@@ -549,6 +549,13 @@ static int attend_tokens(conf_kv_handle *h, int32_t layer, int32_t tq, const voi
     constexpr int64_t kMostStride = (int64_t)1 << 40;
     if (!diff->lambda || ((uintptr_t)diff->lambda & 3) || h->cv.G % 2 || tq * h->cv.G > kChunkRows) return CONF_KV_ERR_INVALID_ARG;
     if (diff->batch_stride < 0 || diff->token_stride < 0 || diff->batch_stride > kMostStride || diff->token_stride > kMostStride) return CONF_KV_ERR_INVALID_ARG;
+    // A unit writes half as many rows as it reads: an output in the queries' place would reach into another unit's.
+    const size_t token = (size_t)h->cfg.head_dim * 2, tokens = (size_t)h->cfg.batch * tq;
+    const size_t q_bytes = tokens * h->cfg.n_q_heads * token, new_bytes = tokens * h->cfg.n_kv_heads * token;
+    const size_t weights = ((h->cfg.batch - 1) * (size_t)diff->batch_stride + (tq - 1) * (size_t)diff->token_stride + h->cfg.n_q_heads / 2) * 4;
+    const struct { const void *at; size_t bytes; } read[] = {{dev_q16, q_bytes}, {dev_knew16, new_bytes}, {dev_vnew16, new_bytes}, {diff->lambda, weights}};
+    for (const auto &r : read)
+      if (overlap(dev_out16, q_bytes / 2, r.at, r.bytes)) return CONF_KV_ERR_INVALID_ARG;
     if (!on_its_device(h)) return CONF_KV_ERR_INVALID_ARG;
   }
   const bool shared = prefix && prefix->tokens > 0;
