@@ -365,7 +365,7 @@ typedef struct conf_kv_chunk {
  * and in no other.  Rows that no sequence claims are left as they were; two sequences claim no row and write to no page together
  * (pages that both only read are shared freely).
  * CONF_KV_ERR_INVALID_ARG beyond the limits noted above, where max_pages * page_tokens is more than max_paged (rounded up to whole
- * pages), and for tensors that overlap what is written (keys and values may take turns in one tensor, not share all of it).
+ * pages), and for tensors that overlap what is written (keys and values may take turns in one tensor, not share a value of it).
  * Tensors are 16-byte aligned, tokens * n_q_heads * B at most 2^30. */
 int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const conf_kv_chunk *chunk, conf_kv_stream stream);
 

@@ -12,6 +12,7 @@
 #include "conf_kv.h"
 #include "confkv_dev.h"
 #include "launch.h"
+#include "pages_layout.h"
 
 using namespace confkv;
 
@@ -349,18 +350,14 @@ static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 }
 
 // Values from the first to the last of the pages' rows; 0 where rows overlap or a size or stride is out of bounds.
-static long long pages_extent(const conf_kv_handle *h, const conf_kv_pages &p) {
-  constexpr int64_t kMostStride = (int64_t)1 << 40;
-  struct Dim { long long size, stride; } d[3] = {{p.n_pages, p.page_stride}, {p.page_tokens, p.token_stride}, {h->cfg.n_kv_heads, p.head_stride}};
-  std::sort(d, d + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride || (x.stride == y.stride && x.size < y.size); });
-  long long extent = h->cfg.head_dim;
-  for (const Dim &x : d) {
-    if (x.stride < 0 || x.stride > kMostStride || x.stride % 8) return 0;
-    if (x.size == 1) continue;
-    if (x.stride < extent || x.size > ((long long)1 << 56) / x.stride) return 0;
-    extent += (x.size - 1) * x.stride;
-  }
-  return extent;
+struct PagesRows {
+  PagesDim d[3];
+  long long extent;
+};
+static PagesRows pages_rows(const conf_kv_handle *h, const conf_kv_pages &p) {
+  PagesRows r = {{{p.n_pages, p.page_stride}, {p.page_tokens, p.token_stride}, {h->cfg.n_kv_heads, p.head_stride}}, 0};
+  r.extent = pages_extent(r.d, h->cfg.head_dim);
+  return r;
 }
 static bool pages_ok(const conf_kv_handle *h, const conf_kv_pages &p) {
   if (!p.dev_k16 || !p.dev_v16 || !p.dev_table) return false;
@@ -368,7 +365,7 @@ static bool pages_ok(const conf_kv_handle *h, const conf_kv_pages &p) {
   if (p.page_tokens < 8 || p.page_tokens > 1 << 20 || (p.page_tokens & (p.page_tokens - 1))) return false;
   if (p.n_pages < 1 || p.n_pages > 1 << 30 || p.max_pages < 1 || (long long)p.max_pages * p.page_tokens > 1ll << 30) return false;
   if (p.table_stride < p.max_pages || p.table_stride > ((int64_t)1 << 56) / h->cfg.batch) return false;
-  return pages_extent(h, p) > 0;
+  return pages_rows(h, p).extent > 0;
 }
 static PagesView pages_view(const conf_kv_pages &p) {
   PagesView v{};
@@ -434,7 +431,8 @@ int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const co
   if (((uintptr_t)c.dev_starts | (uintptr_t)c.dev_new | (uintptr_t)c.dev_context | (uintptr_t)c.dev_lambda) & 3) return CONF_KV_ERR_INVALID_ARG;
   if (c.dev_lambda && (G % 2 || c.lambda_stride < 0 || c.lambda_stride > ((int64_t)1 << 56) / c.rows)) return CONF_KV_ERR_INVALID_ARG;
   const size_t q_bytes = (size_t)c.rows * Hq * D * 2, new_bytes = (size_t)c.rows * H * D * 2, out_bytes = c.dev_lambda ? q_bytes / 2 : q_bytes;
-  const size_t page_bytes = (size_t)pages_extent(h, *pages) * 2;
+  const PagesRows page_rows = pages_rows(h, *pages);
+  const size_t page_bytes = (size_t)page_rows.extent * 2;
   if (overlap(c.dev_out16, out_bytes, c.dev_q16, q_bytes)) return CONF_KV_ERR_INVALID_ARG;
   for (const void *plane : {pages->dev_k16, pages->dev_v16}) {
     if (overlap(c.dev_out16, out_bytes, plane, page_bytes)) return CONF_KV_ERR_INVALID_ARG;
@@ -442,7 +440,7 @@ int conf_kv_attend_pages(conf_kv_handle *h, const conf_kv_pages *pages, const co
       if (fresh && (overlap(fresh, new_bytes, plane, page_bytes) || overlap(fresh, new_bytes, c.dev_out16, out_bytes))) return CONF_KV_ERR_INVALID_ARG;
     if (c.dev_knew16 && overlap(c.dev_q16, q_bytes, plane, page_bytes)) return CONF_KV_ERR_INVALID_ARG;
   }
-  if (c.dev_knew16 && pages->dev_k16 == pages->dev_v16) return CONF_KV_ERR_INVALID_ARG;
+  if (c.dev_knew16 && planes_meet(page_rows.d, D, ((const char *)pages->dev_v16 - (const char *)pages->dev_k16) / 2)) return CONF_KV_ERR_INVALID_ARG;
   const struct { const void *at; size_t bytes; } read[] = {                       // what tells the rows and their weights apart
       {c.dev_starts, (size_t)B * 4}, {c.dev_new, (size_t)B * 4}, {c.dev_context, (size_t)B * 4},
       {pages->dev_table, ((size_t)(B - 1) * pages->table_stride + pages->max_pages) * 4},

@@ -48,3 +48,29 @@ def test_output_of_differences_inside_its_inputs(lib, torch, tq):
         kv.attend_diff(0, q, k, v, out, out.view(torch.float32).reshape(-1)[64:64 + G * H // 2])
     assert kv.counters().device_errors == 0
     kv.close()
+
+
+def test_planes_of_pages_that_share_some_values(lib, torch):
+    """Keys and values may take turns in one tensor; where a row of one reaches into a row of the other they are refused, unless
+    nothing is written."""
+    B, H, G, D, page, n = 2, 2, 2, 128, 16, 6
+    kv = lib.ConfKV(n_layers=1, batch=B, n_q_heads=G * H, n_kv_heads=H, head_dim=D, vocab=100, capacity=64, fp16_window=16,
+                    protected_window=16, n_tight=[32], n_loose=[32], max_paged=4 * page)
+    t = lambda *s, d=torch.float16: torch.zeros(s, dtype=d, device="cuda")
+    q, k, v, out = t(B, 2, G * H, D), t(B, 2, H, D), t(B, 2, H, D), t(B, 2, G * H, D)
+    table, context = t(B, 4, d=torch.int32), t(B, d=torch.int32)
+    table[1] = 4
+    plane = page * H * D
+    room = t(4 * n * plane)
+    for strides, turn in (((2 * plane, H * D, D), plane), ((2 * plane, 2 * H * D, D), H * D), ((2 * plane, 2 * H * D, 2 * D), D),
+                          ((plane, H * D, D), n * plane)):
+        view = lambda at: room[at:].as_strided((n, page, H, D), strides + (1,), room.storage_offset() + at)
+        kv.attend_pages(q, k, v, out, view(0), view(turn), table, context)
+        kv.attend_pages(q, k, v, out, view(turn), view(0), table, context)
+        for off in (0, 8, turn - 8, turn - D + 8):
+            for pair in ((0, off), (off, 0)):
+                with pytest.raises(lib.ConfKVError) as e:
+                    kv.attend_pages(q, k, v, out, *(view(x) for x in pair), table, context)
+                assert e.value.status == lib.binding.ERR_INVALID_ARG
+                kv.attend_pages(q, None, None, out, *(view(x) for x in pair), table, context)
+    kv.close()
