@@ -320,7 +320,7 @@ class ConfKV:
         in memory with dense heads) with table int32 [B][pages per sequence], in which sequence b has context[b] tokens (int32 [B]).
         q16 [B][T][Hq][D], knew16 / vnew16 [B][T][Hkv][D] (None: the pages hold them); or rows [R][..][D] of which sequence b has
         starts[b] .. starts[b] + new[b] - 1 (int32 [B]), at most `tokens` of them.  out16 [..][Hq][D], with
-        lam float32 [..][Hq / 2] or [Hq / 2], the weights of the second maps, [..][Hq / 2][D]."""
+        lam float32 [..][Hq / 2] or [Hq / 2], the weights of the second maps (a slice of wider rows will do), [..][Hq / 2][D]."""
         B, H, Hq, D, want, half, i32 = self._batch, self._kv_heads, self._q_heads, self._head_dim, self._want, self._half, self._i32
         shape = q16.shape
         outs, weights, apart = Hq, 0, 0
@@ -339,15 +339,26 @@ class ConfKV:
             raise ValueError(f"q16: [{B}][T][{Hq}][{D}], with `starts` for fewer tokens than T, or [R][{Hq}][{D}] with `starts` and `tokens` "
                              f"is wanted, got {tuple(shape)} with {tokens} tokens")
         if lam is not None:
-            if lam.shape == (outs,):
-                weights = want("lam", lam, self._f32, (outs,))
-            else:
-                weights, apart = want("lam", lam, self._f32, given[:-1]), outs
+            weights, apart = self._weights(lam, given[:-1])
         chunk = _CHUNK.pack(tokens, rows, want("starts", starts, i32, (B,)), want("new", new, i32, (B,)), want("context", context, i32, (B,)),
                             want("q16", q16, half, like), want("knew16", knew16, half, fresh), want("vnew16", vnew16, half, fresh),
                             want("out16", out16, half, given), weights, apart)
         return self._check(self.lib.conf_kv_attend_pages(self.h, self._pages(pages_k, pages_v, table), chunk, self._current_stream()),
                            "conf_kv_attend_pages")
+
+    def _weights(self, lam, shape):
+        """Address of float32 weights [pairs] or [..][pairs] of all rows, and how many values their rows lie apart: one distance for
+        all of them, dense pairs (a size of 1 may come with any stride)."""
+        pairs, step = shape[-1], lam.stride()
+        if lam.dtype is self._f32 and lam.get_device() == self._device and (step[-1:] == (1,) or pairs == 1):
+            if lam.shape == (pairs,):
+                return lam.data_ptr(), 0
+            if lam.shape == shape:
+                apart = step[-2] if shape[-2] > 1 else step[0] if len(shape) == 3 else pairs
+                if len(shape) == 2 or shape[0] == 1 or shape[1] <= 1 or step[0] == shape[1] * apart:
+                    return lam.data_ptr(), apart
+        raise ValueError(f"lam: float32 [{pairs}] or {list(shape)} with dense pairs and rows equally far apart on {self.state.device} is wanted, "
+                         f"got {lam.dtype} {tuple(lam.shape)} strides {step} on {lam.device}")
 
     def load_pages(self, layer: int, pages_k, pages_v, table, tokens: int, ema0=None):
         """load_prefill of the first `tokens` tokens of every sequence from pages (see attend_pages)."""
