@@ -361,8 +361,9 @@ typedef struct conf_kv_chunk {
  * with float32 accumulation.  With dev_lambda, differential attention: heads 2 j and 2 j + 1 of a kv-head's group are the two maps
  * of pair j, the output is their difference sum_i (p_i - lambda p'_i) V_i (conf_kv_attend_diff).
  * The handle gives B, Hq, Hkv, D and the softmax scale; nothing of its cache changes, and the lengths are the caller's, on the
- * device: a recorded call moves on with them.  A token's key that is infinite or NaN shows in the rows that see it
- * and in no other.  Rows that no sequence claims are left as they were; two sequences claim no row and write to no page together
+ * device: a recorded call moves on with them.  A token's key that is NaN or scores +infinity leaves no
+ * number in the rows that see it (one that scores -infinity has no weight), a value that is none shows in its channel of these rows; no other
+ * row shows either.  Rows that no sequence claims are left as they were; two sequences claim no row and write to no page together
  * (pages that both only read are shared freely).
  * CONF_KV_ERR_INVALID_ARG beyond the limits noted above, where max_pages * page_tokens is more than max_paged (rounded up to whole
  * pages), and for tensors that overlap what is written (keys and values may take turns in one tensor, not share a value of it).
