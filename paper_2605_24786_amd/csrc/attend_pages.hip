@@ -760,13 +760,13 @@ __device__ __forceinline__ constexpr int pg_swizzle(int r) {
 }
 // Sixteen bytes per lane from the lane's address to LDS bytes [to, to + 1024), lane by lane.
 __device__ __forceinline__ void pg_load_lds(const void *from, unsigned to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
 }
 // The same from `from`, alike in all lanes, plus the lane's offset in bytes.
 __device__ __forceinline__ void pg_load_lds(const void *from, unsigned offset, unsigned to) {
   const unsigned long long p = (unsigned long long)from;
   const unsigned long long at = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)p);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(at) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(at) : "memory", "m0");
 }
 __device__ __forceinline__ unsigned pg_lds_at(const void *p) {
   return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
