@@ -1058,6 +1058,7 @@ __global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a
 // Slots of a split call: as many as there are workgroups on the chip at a time, one of many rows to a compute unit or two of few (with
 // twice as many 8 tokens behind 2000 took 25.8 us instead of 20.9, 32 behind 600 27.3 instead of 24.0).
 constexpr int kManySlots = 256, kFewSlots = 512;
+static_assert(kFewSlots <= kPagesCounters, "a block's counter is that of its first part's slot");
 constexpr size_t kSlotRows = std::max(kManySlots * kManyRows, kFewSlots * kPgRows);
 size_t pages_scratch_floats(int D) { return kSlotRows * (D + 2); }
 
