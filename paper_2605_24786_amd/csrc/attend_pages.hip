@@ -260,7 +260,7 @@ struct PgRows {
   // that only wavefronts with such a row run (`far`).
   float off, ref, limit, l;                            // limit: the score beyond which the reference moves
   bool far;
-  int row, lim, least, most;                           // row of the block; keys the lane's row sees; the fewest and the most
+  int lim, least, most;                                // keys the lane's row sees; the fewest and the most
 
   static constexpr float kLift = 10.f, kSlack = 5.5f;  // 2^15.5 is 46341 of fp16's 65504
   static constexpr float kFar = 0x1p20f;               // off within 2^-3 of what it is meant to be
@@ -279,16 +279,13 @@ struct PgRows {
   // rows first .. first + 31 of the sequence's n * G
   __device__ __forceinline__ void init(const PagesLaunch &a, const PgJob &j, int first) {
     const int lane = threadIdx.x & 63, h = lane >> 5, all = j.q.n * a.G;
-    row = first + (lane & 31);
-    const bool real = row < all;
-    const int r = min(row, all - 1), t = pg_token(a, r), hq = r - t * a.G;
+    const int r = min(first + (lane & 31), all - 1), t = pg_token(a, r), hq = r - t * a.G;
     const __half *q = a.q + ((long long)(j.q.s + t) * a.Hkv * a.G + j.g * a.G + hq) * D;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) qf[s] = __builtin_bit_cast(pg_h8, *(const int4 *)(q + 16 * s + 8 * h));
     lim = j.q.c + t + 1;
     least = __builtin_amdgcn_readfirstlane(lim);       // (rows in order: the first sees least)
     most = first < all ? __builtin_amdgcn_readlane(lim, 31) : 0;
-    row = real ? row : -1;
     reset();
   }
   template <int KROW>
