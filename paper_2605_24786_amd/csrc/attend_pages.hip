@@ -755,15 +755,16 @@ template <int D>
 __device__ __forceinline__ constexpr int pg_swizzle(int r) {
   return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
-// Sixteen bytes per lane from the lane's address to LDS bytes [to, to + 1024), lane by lane.
+// Sixteen bytes per lane from the lane's address to LDS bytes [to, to + 1024), lane by lane.  (m0, which holds `to`, is an operand that the
+// compiler writes, so that it knows what became of its own; the load may follow that write by one wait state at the least.)
 __device__ __forceinline__ void pg_load_lds(const void *from, unsigned to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
 // The same from `from`, alike in all lanes, plus the lane's offset in bytes.
 __device__ __forceinline__ void pg_load_lds(const void *from, unsigned offset, unsigned to) {
   const unsigned long long p = (unsigned long long)from;
   const unsigned long long at = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)p);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(at) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(at) : "memory");
 }
 __device__ __forceinline__ unsigned pg_lds_at(const void *p) {
   return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
