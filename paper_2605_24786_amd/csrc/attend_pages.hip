@@ -739,7 +739,8 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 // ---------------------------------------------------------------------------------------
 // More rows: bound by the matrix products and the exponentials, and in the end by power.  Eight wavefronts of 32 rows each share tiles
 // of 64 keys in three buffers, one barrier per tile; the tile after the next is on its way.
-// Four prompts of 8192 tokens (32 heads, 8 kv-heads, 128 channels): 2.20 ms, 1000 TFLOP/s where a large library product reaches 1136.  The
+// Four prompts of 8192 tokens (32 heads, 8 kv-heads, 128 channels): 2.20 ms, 1000 TFLOP/s where a large library product reaches 1136 (other
+// cards take up to 2.46: the clock that their power leaves).  The
 // matrix units are busy in 48 % of the cycles and the vector units in 47 %, at 1.68 of 2.4 GHz.  On the way: tiles through registers
 // with padded rows 3.75 ms; straight into LDS 2.57; addresses of whole tiles from scalars 2.51; scores a step ahead 2.46 (before: four
 // wavefronts and two buffers, two workgroups to a unit).  64 rows a wavefront, which halves the reads of the tiles, leave one wavefront
@@ -1053,7 +1054,7 @@ __global__ __launch_bounds__(kManyThreads) void pages_merge_kernel(PagesLaunch a
 // ---------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------
-// Slots of a split call: as many as there are workgroups on the chip at a time, one of many rows to a compute unit or two of few (with
+// Slots of a split call: as many as there are workgroups on the chip (256 compute units) at a time, one of many rows to a unit or two of few (with
 // twice as many 8 tokens behind 2000 took 25.8 us instead of 20.9, 32 behind 600 27.3 instead of 24.0).
 constexpr int kManySlots = 256, kFewSlots = 512;
 static_assert(kFewSlots <= kPagesCounters, "a block's counter is that of its first part's slot");
